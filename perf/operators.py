@@ -1,0 +1,391 @@
+"""The operators of an autoregressive serving step as measurable cases: attention of new tokens over a paged cache, the block
+quantiser and the block-scaled FP8 product, and the adjustment of logits in front of the selection.
+
+A case is a dict of plain values.  listed() names the cases, draw() gives further ones of the same ranges, prepare() makes what a
+serving process has in hand before the call, run() is one call - in elementary torch operations, or, with `own` true, through the
+framework's entry points - work() the bytes and operations it cannot do without, exact() the result in 64 bits.
+"""
+import math
+
+import torch
+
+own = False
+
+F8 = torch.float8_e4m3fn
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+
+
+# ---- cases ------------------------------------------------------------------------------------------------------------
+def _attention(name, dtype, B, new, length, H, H_kv, dh, page, window=0, sinks=0):
+    """new, length: (least, most) new tokens of a sequence, and tokens it has with them."""
+    return {"name": name, "op": "attention", "dtype": dtype, "B": B, "new_lo": new[0], "new_hi": new[1], "len_lo": length[0], "len_hi": length[1],
+            "H": H, "H_kv": H_kv, "dh": dh, "page": page, "window": window, "sinks": sinks}
+
+
+def _quantize(name, dtype, rows, n, block_rows):
+    return {"name": name, "op": "quantize", "dtype": dtype, "rows": rows, "n": n, "block_rows": block_rows}
+
+
+def _linear(name, M, N, K, out, bias):
+    return {"name": name, "op": "linear", "M": M, "N": N, "K": K, "out": out, "bias": bias}
+
+
+def _logits(name, dtype, rows, V, history, masks, biases, penalties):
+    """history: most earlier tokens of a row; masks, biases: rows of those tables (0: none)."""
+    return {"name": name, "op": "logits", "dtype": dtype, "rows": rows, "V": V, "history": history, "masks": masks, "biases": biases, "penalties": penalties}
+
+
+def listed():
+    return [
+        # an interactive call: the next token of one sequence
+        _attention("attention-one", "bf16", 1, (1, 1), (777, 777), 16, 4, 64, 16),
+        # a serving batch, one token for every sequence, ragged lengths, shared heads
+        _attention("attention-decode", "bf16", 64, (1, 1), (512, 8192), 32, 8, 128, 64),
+        # two very long sequences, one token each: few rows over a long axis
+        _attention("attention-long", "bf16", 2, (1, 1), (100001, 131072), 32, 8, 128, 64),
+        # a prompt's chunks: many new tokens over what the cache holds already
+        _attention("attention-chunk", "bf16", 4, (1000, 1024), (1024, 8192), 32, 8, 128, 64),
+        # a mixed batch in float32 under a sliding window with first tokens that stay visible: single tokens beside short chunks
+        _attention("attention-window", "f32", 32, (1, 96), (96, 12000), 16, 2, 64, 32, window=1024, sinks=4),
+        # activations of a few thousand rows in front of an FP8 product
+        _quantize("quantize-activations", "bf16", 4096, 4096, 1),
+        # a classifier's weights, once per weight refresh; an odd width
+        _quantize("quantize-weights", "f32", 16384, 1040, 128),
+        # a projection for the single tokens of a small batch: the weights are what is read
+        _linear("linear-few", 5, 4096, 1024, "bf16", False),
+        # a classifier of odd size over a mid-size batch's rows, logits in half precision for the selection
+        _linear("linear-odd", 517, 1000, 1104, "f16", True),
+        # a wide projection of many rows
+        _linear("linear-large", 16384, 4096, 4096, "bf16", False),
+        # the beams of a few requests in front of the selection: latency
+        _logits("logits-few", "f32", 64, 1024, 8, 16, 1, True),
+        # a wide level of a batch: half-precision logits, a mask for every prefix, popularity biases
+        _logits("logits-beams", "f16", 16384, 8192, 64, 512, 4, True),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["attention", "attention", "quantize", "linear", "logits"])
+    while True:
+        if op == "attention":
+            dtype = rng.choice(["bf16", "bf16", "f32"])
+            dh, group = rng.choice([32, 64, 64, 128, 128]), rng.choice([1, 2, 4, 8])
+            H = group * rng.choice([1, 2, 4, 8])
+            kind = rng.choice(["single", "chunk", "mixed"])
+            B, most = _log(rng, 1, 96), _log(rng, 1, 100000)
+            hi = {"single": 1, "chunk": _log(rng, 16, 1024), "mixed": _log(rng, 2, 128)}[kind]
+            lo = hi if kind != "mixed" else 1
+            window = rng.choice([0, 0, _log(rng, 16, 4096)])
+            c = _attention("", dtype, B, (lo, hi), (max(1, most // rng.choice([1, 2, 8])), most), H, H // group, dh, rng.choice([16, 32, 64, 128]), window,
+                           rng.choice([0, 1, 4, 64]) if window else 0)
+            w, padded = work(c), B * H * hi * most  # (the plain form's scores)
+            if w["bytes"] <= 1.2e9 and w["flops"] <= 3e11 * (0.1 if dtype == "f32" else 1) and padded <= 1.2e9 and B * most * H // group * dh <= 3e8:
+                break
+        elif op == "quantize":
+            c = _quantize("", rng.choice(["bf16", "f32"]), _log(rng, 1, 16384), _log(rng, 16, 16384), rng.choice([1, 1, 128]))
+            if c["rows"] * c["n"] <= 1 << 26:
+                break
+        elif op == "linear":
+            K = 16 * _log(rng, 8, 512) if rng.random() < 0.8 else _log(rng, 100, 2000)
+            c = _linear("", _log(rng, 1, 16384), _log(rng, 64, 16384), K, rng.choice(["bf16", "f16"]), rng.random() < 0.5)
+            if 2.0 * c["M"] * c["N"] * K <= (5e11 if K % 16 == 0 else 5e9):
+                break
+        else:
+            V = _log(rng, 100, 160000)
+            c = _logits("", rng.choice(["f32", "f16"]), _log(rng, 1, 16384), V, rng.choice([0, _log(rng, 1, 4096)]), rng.choice([0, _log(rng, 1, 1024)]), rng.choice([0, 1, 3]),
+                        rng.random() < 0.8)
+            if c["rows"] * V <= 1 << 27 and c["rows"] * c["history"] <= 1 << 23 and c["masks"] * V <= 1 << 27:
+                break
+    del c["name"]
+    return c
+
+
+# ---- inputs -----------------------------------------------------------------------------------------------------------
+def _lengths(c):
+    """(new tokens, tokens) of every sequence: evenly spread over their ranges."""
+    B = c["B"]
+    at = lambda lo, hi, i: lo + (hi - lo) * i // max(1, B - 1)  # noqa: E731
+    new = [at(c["new_lo"], c["new_hi"], i * 7 % B if math.gcd(7, B) == 1 else i) for i in range(B)]
+    return new, [max(m, at(c["len_lo"], c["len_hi"], i)) for i, m in enumerate(new)]
+
+
+def _randn(g, *shape, dtype=torch.float32):
+    return torch.randn(*shape, device="cuda", generator=g, dtype=dtype)
+
+
+def _prepare_attention(c, g):
+    td, B, H, H_kv, dh, page = TYPES[c["dtype"]], c["B"], c["H"], c["H_kv"], c["dh"], c["page"]
+    new, lens = _lengths(c)
+    order = torch.randperm(B, device="cuda", generator=g).cpu().tolist()
+    new, lens = [new[i] for i in order], [lens[i] for i in order]
+    starts = [0]
+    for m in new:
+        starts.append(starts[-1] + m)
+    per = [-(-n // page) for n in lens]
+    n_pages, max_pages = sum(per) + 3, max(per)
+    ids = torch.randperm(n_pages, device="cuda", generator=g).to(torch.int32)
+    table, at = torch.zeros(B, max_pages, dtype=torch.int32, device="cuda"), 0
+    for b, n in enumerate(per):
+        table[b, :n] = ids[at:at + n]
+        at += n
+    N = starts[-1]
+    qkv = _randn(g, N, (H + 2 * H_kv) * dh, dtype=td)  # one projection's output: the parts are views of it
+    q, k_new, v_new = qkv[:, :H * dh].view(N, H, dh), qkv[:, H * dh:(H + H_kv) * dh].view(N, H_kv, dh), qkv[:, (H + H_kv) * dh:].view(N, H_kv, dh)
+    s = {"q": q, "k_new": k_new, "v_new": v_new, "table": table, "start": torch.tensor(starts, dtype=torch.int32, device="cuda"),
+         "len": torch.tensor(lens, dtype=torch.int32, device="cuda"), "k_pages": _randn(g, n_pages, H_kv, page, dh, dtype=td),
+         "v_pages": _randn(g, n_pages, H_kv, dh, page, dtype=td), "most_new": max(new), "out": torch.empty(N, H, dh, dtype=td, device="cuda")}
+    return s
+
+
+def _quantized(x, block_rows):
+    """E4M3 values and scales [blocks along n, blocks along rows] of x, in float32 operations."""
+    rows, n = x.shape
+    rb, nb = -(-rows // block_rows), -(-n // 128)
+    padded = torch.nn.functional.pad(x.float(), (0, nb * 128 - n, 0, rb * block_rows - rows)).view(rb, block_rows, nb, 128)
+    amax = padded.abs().amax(dim=(1, 3))
+    zero = amax < 2.0 ** -100
+    inv = torch.where(zero, 1.0, 448.0 / amax)
+    q = (padded * inv[:, None, :, None]).to(F8).view(rb * block_rows, nb * 128)[:rows, :n]
+    return q.contiguous(), torch.where(zero, 1.0, amax / 448.0).t().contiguous()
+
+
+def _activations(g, rows, n, dtype):
+    """Values as a normalised layer leaves them: a few columns are far larger than the rest."""
+    x = _randn(g, rows, n)
+    x *= torch.where(torch.rand(n, device="cuda", generator=g) < 0.01, 20.0, 1.0)
+    return x.to(dtype)
+
+
+def _prepare_linear(c, g):
+    M, N, K = c["M"], c["N"], c["K"]
+    aq, a_scale = _quantized(_activations(g, M, K, torch.bfloat16), 1)
+    wq, w_scale = _quantized((_randn(g, N, K) / math.sqrt(K)).to(torch.bfloat16), 128)
+    return {"aq": aq.view(torch.uint8), "a_scale": a_scale, "wq": wq.view(torch.uint8), "w_scale": w_scale, "bias": _randn(g, N) if c["bias"] else None}
+
+
+def _prepare_logits(c, g):
+    R, V = c["rows"], c["V"]
+    uniform = lambda lo, hi: lo + (hi - lo) * torch.rand(R, device="cuda", generator=g)  # noqa: E731
+    below = lambda n, *shape: torch.randint(0, n, shape, device="cuda", generator=g, dtype=torch.int32)  # noqa: E731
+    s = {"logits": (2.0 * _randn(g, R, V)).to(TYPES[c["dtype"]]), "history": None, "history_len": None, "repetition": None, "presence": None, "frequency": None,
+         "bias": None, "bias_row": None, "mask": None, "mask_row": None}
+    if c["history"]:
+        s["history"] = (below(V, R, c["history"]).float() * torch.rand(R, c["history"], device="cuda", generator=g)).to(torch.int32)  # popular tokens: low ones
+        s["history_len"] = below(c["history"] + 1, R)
+        s["frequency"] = uniform(0.0, 0.2)
+        if c["penalties"]:
+            s["repetition"], s["presence"] = uniform(1.0, 1.4), uniform(-0.2, 0.6)
+    if c["biases"]:
+        s["bias"] = _randn(g, c["biases"], V)
+        s["bias_row"] = below(c["biases"] + 1, R) - 1  # (-1: none)
+    if c["masks"]:
+        words = (c["masks"], -(-V // 32))
+        s["mask"] = below(1 << 16, *words) << 16 | below(1 << 16, *words)
+        s["mask"][-1] = 0  # a prefix that nothing may follow
+        s["mask_row"] = below(c["masks"] + 1, R) - 1
+    return s
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(int(seed))
+    if case["op"] == "attention":
+        s = _prepare_attention(case, g)
+    elif case["op"] == "quantize":
+        s = {"x": _activations(g, case["rows"], case["n"], TYPES[case["dtype"]])}
+    elif case["op"] == "linear":
+        s = _prepare_linear(case, g)
+    else:
+        s = _prepare_logits(case, g)
+    s["case"] = dict(case)
+    return s
+
+
+# ---- plain forms ------------------------------------------------------------------------------------------------------
+def _plain_attention(c, s):
+    q, table, start, lens = s["q"], s["table"].long(), s["start"].long(), s["len"].long()
+    B, H, H_kv, dh, page, m = c["B"], c["H"], c["H_kv"], c["dh"], c["page"], s["most_new"]
+    N, new = q.shape[0], start[1:] - start[:-1]
+    seq = torch.repeat_interleave(torch.arange(B, device="cuda"), new, output_size=N)
+    at = torch.arange(N, device="cuda") - start[seq] + (lens - new)[seq]  # position of every row
+    ids = table[seq, at // page]
+    s["k_pages"][ids, :, at % page] = s["k_new"]
+    s["v_pages"][ids, :, :, at % page] = s["v_new"]
+    keys = s["k_pages"][table].permute(0, 2, 1, 3, 4).reshape(B, H_kv, -1, dh).float()
+    values = s["v_pages"][table].permute(0, 2, 3, 1, 4).reshape(B, H_kv, dh, -1).float()
+    L = keys.shape[2]
+    rows = (start[:-1, None] + torch.arange(m, device="cuda")).clamp(max=N - 1)  # [B, m], ragged ends repeat a row
+    qs = q[rows].float().view(B, m, H_kv, H // H_kv, dh).permute(0, 2, 3, 1, 4).reshape(B, H_kv, -1, dh)
+    scores = (qs @ keys.transpose(2, 3)) * (1.0 / math.sqrt(dh))
+    pos, j = (lens - new)[:, None, None] + torch.arange(m, device="cuda")[None, :, None], torch.arange(L, device="cuda")
+    seen = (j <= pos) & (j < lens[:, None, None])
+    if c["window"]:
+        seen &= (pos - j < c["window"]) | (j < c["sinks"])
+    scores = scores.view(B, H_kv, H // H_kv, m, L).masked_fill_(~seen[:, None, None], -math.inf)
+    p = scores.sub_(scores.amax(dim=-1, keepdim=True)).exp_()
+    p = (p / p.sum(dim=-1, keepdim=True)).view(B, H_kv, -1, L)
+    o = (p @ values.transpose(2, 3)).view(B, H_kv, H // H_kv, m, dh).permute(0, 3, 1, 2, 4).reshape(B, m, H, dh)
+    s["out"][:] = o[seq, torch.arange(N, device="cuda") - start[seq]].to(q.dtype)
+    return s["out"]
+
+
+def _dequantized(q, scale, block_rows):
+    rows, n = q.shape
+    full = scale.t().repeat_interleave(128, dim=1)[:, :n].repeat_interleave(block_rows, dim=0)[:rows]
+    return q.view(F8).to(scale.dtype) * full
+
+
+def _plain_linear(c, s):
+    y = _dequantized(s["aq"], s["a_scale"], 1) @ _dequantized(s["wq"], s["w_scale"], 128).t()
+    if s["bias"] is not None:
+        y = y + s["bias"]
+    return y.to(TYPES[c["out"]])
+
+
+def _plain_logits(s):
+    R, V = s["logits"].shape
+    x = s["logits"].float()
+    if s["history"] is not None:
+        kept = torch.arange(s["history"].shape[1], device="cuda") < s["history_len"][:, None]
+        count = torch.zeros(R, V + 1, device="cuda").scatter_add_(1, torch.where(kept, s["history"], V).long(), kept.float())[:, :V]
+        if s["repetition"] is not None:
+            x = torch.where(count > 0, torch.where(x > 0, x / s["repetition"][:, None], x * s["repetition"][:, None]), x)
+        x = x - s["frequency"][:, None] * count
+        if s["presence"] is not None:
+            x = x - s["presence"][:, None] * (count > 0)
+    if s["bias"] is not None:
+        x = x + torch.where(s["bias_row"][:, None] >= 0, s["bias"][s["bias_row"].clamp(min=0).long()], 0.0)
+    if s["mask"] is not None:
+        v = torch.arange(V, device="cuda")
+        allowed = (s["mask"][s["mask_row"].clamp(min=0).long()][:, v // 32] >> (v % 32)) & 1
+        x = torch.where((allowed == 0) & (s["mask_row"][:, None] >= 0), -math.inf, x)
+    return x.to(s["logits"].dtype)
+
+
+def run(state):
+    c, s = state["case"], state
+    if own:
+        from paper_2602_22732_amd import binding
+        if c["op"] == "attention":
+            out = binding.op_paged_attention(s["q"], s["k_pages"], s["v_pages"], s["table"], s["start"], s["len"], k_new=s["k_new"], v_new=s["v_new"],
+                                             window=c["window"], sinks=c["sinks"], out=s["out"])
+            return {"out": out, "k_pages": s["k_pages"], "v_pages": s["v_pages"]}
+        if c["op"] == "quantize":
+            q, scale = binding.op_quantize_blocks(s["x"], c["block_rows"])
+            return {"q": q.view(F8), "scale": scale}
+        if c["op"] == "linear":
+            return binding.op_linear_fp8_block(s["aq"], s["a_scale"], s["wq"], s["w_scale"], bias=s["bias"], out_dtype=TYPES[c["out"]])
+        return binding.op_adjust_logits(s["logits"], history=s["history"], history_len=s["history_len"], repetition=s["repetition"], presence=s["presence"],
+                                        frequency=s["frequency"], bias=s["bias"], bias_row=s["bias_row"], mask=s["mask"], mask_row=s["mask_row"])
+    if c["op"] == "attention":
+        return {"out": _plain_attention(c, s), "k_pages": s["k_pages"], "v_pages": s["v_pages"]}
+    if c["op"] == "quantize":
+        q, scale = _quantized(s["x"], c["block_rows"])
+        return {"q": q, "scale": scale}
+    if c["op"] == "linear":
+        return _plain_linear(c, s)
+    return _plain_logits(s)
+
+
+# ---- what a call cannot do without --------------------------------------------------------------------------------------
+def work(case):
+    c = case
+    if c["op"] == "attention":
+        new, lens = _lengths(c)
+        e, w, first = SIZE[c["dtype"]], c["window"], c["sinks"]
+        keys = pairs = 0
+        for m, n in zip(new, lens):
+            if not w:
+                keys += n
+                pairs += m * n - m * (m - 1) // 2
+            else:
+                keys += min(n, w + m - 1 + first)
+                pairs += sum(min(p + 1, w) + min(first, max(0, p + 1 - w)) for p in range(n - m, n))
+        row = c["dh"] * e
+        return {"bytes": float(2 * keys * c["H_kv"] * row + sum(new) * (2 * c["H"] + 4 * c["H_kv"]) * row), "flops": 4.0 * pairs * c["H"] * c["dh"]}
+    if c["op"] == "quantize":
+        return {"bytes": float(c["rows"] * c["n"] * (SIZE[c["dtype"]] + 1) + 4 * -(-c["rows"] // c["block_rows"]) * -(-c["n"] // 128)), "flops": 3.0 * c["rows"] * c["n"]}
+    if c["op"] == "linear":
+        M, N, K = c["M"], c["N"], c["K"]
+        return {"bytes": float((M + N) * K + 2 * M * N + 4 * -(-K // 128) * (M + -(-N // 128)) + 4 * N * c["bias"]), "flops": 2.0 * M * N * K}
+    R, V = c["rows"], c["V"]
+    return {"bytes": float(2 * SIZE[c["dtype"]] * R * V + 2 * R * c["history"] + 4 * V * c["biases"] + 4 * min(c["masks"], R) * -(-V // 32)), "flops": 6.0 * R * V}
+
+
+# ---- 64 bits ------------------------------------------------------------------------------------------------------------
+def _exact_attention(c, s):
+    if work(c)["flops"] > 4e11:
+        return None
+    group, out = c["H"] // c["H_kv"], torch.zeros(s["q"].shape, dtype=torch.float64, device="cuda")
+    starts, lens, page, scale = s["start"].tolist(), s["len"].tolist(), c["page"], c["dh"] ** -0.5
+    for b, n in enumerate(lens):
+        r0, r1 = starts[b], starts[b + 1]
+        m = r1 - r0
+        ids = s["table"][b, :-(-n // page)].long()
+        pos, j = torch.arange(n - m, n, device="cuda")[:, None], torch.arange(n, device="cuda")[None]
+        hidden = j > pos
+        if c["window"]:
+            hidden = hidden | ((pos - j >= c["window"]) & (j >= c["sinks"]))
+        for h in range(c["H_kv"]):
+            k = s["k_pages"][ids, h].double().flatten(0, 1)[:n]
+            v = s["v_pages"][ids, h].double().transpose(1, 2).flatten(0, 1)[:n]
+            k[n - m:], v[n - m:] = s["k_new"][r0:r1, h].double(), s["v_new"][r0:r1, h].double()
+            for i in range(h * group, h * group + group):
+                x = torch.mm(s["q"][r0:r1, i].double(), k.t().contiguous()) * scale
+                x[hidden] = -math.inf
+                out[r0:r1, i] = torch.mm(torch.softmax(x, dim=1), v)
+    return {"out": out, "k_pages": None, "v_pages": None}
+
+
+def _exact_logits(s):
+    x = s["logits"].double()
+    if s["history"] is not None:
+        count = torch.zeros_like(x)
+        ones = torch.ones(1, dtype=torch.float64, device="cuda")
+        i = torch.arange(s["history"].shape[1], device="cuda")[None].expand_as(s["history"])
+        r, i = torch.nonzero(i < s["history_len"][:, None], as_tuple=True)
+        count.index_put_((r, s["history"][r, i].long()), ones.expand(r.numel()), accumulate=True)
+        was = count > 0
+        if s["repetition"] is not None:
+            f = s["repetition"].double()[:, None].expand_as(x)
+            x = torch.where(was & (x > 0), x / f, torch.where(was, x * f, x))
+        x = x - count * s["frequency"].double()[:, None]
+        if s["presence"] is not None:
+            x = x - was.double() * s["presence"].double()[:, None]
+    if s["bias"] is not None:
+        table = torch.cat([torch.zeros_like(s["bias"][:1]), s["bias"]]).double()
+        x = x + table[(s["bias_row"] + 1).long()]
+    if s["mask"] is not None:
+        V = x.shape[1]
+        bits = (s["mask"][:, :, None] >> torch.arange(32, device="cuda")).bitwise_and(1).flatten(1)[:, :V].bool()
+        bits = torch.cat([torch.ones_like(bits[:1]), bits])
+        x[~bits[(s["mask_row"] + 1).long()]] = -math.inf
+    return x
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "attention":
+        return _exact_attention(case, s)
+    if case["op"] == "quantize":
+        x, rows, n = s["x"].double(), case["rows"], case["n"]
+        tall = case["block_rows"]
+        full = torch.zeros(-(-rows // tall) * tall, -(-n // 128) * 128, dtype=torch.float64, device="cuda")
+        full[:rows, :n] = x
+        scale = full.abs().unflatten(0, (-1, tall)).unflatten(2, (-1, 128)).amax(dim=3).amax(dim=1) / 448.0
+        scale[scale == 0] = 1.0
+        return {"q": x / scale.repeat_interleave(tall, 0)[:rows].repeat_interleave(128, 1)[:, :n], "scale": scale.t()}
+    if case["op"] == "linear":
+        a = s["aq"].view(F8).double()
+        w = s["wq"].view(F8).double()
+        for k in range(s["a_scale"].shape[0]):
+            a[:, k * 128:k * 128 + 128] *= s["a_scale"][k].double()[:, None]
+            for j in range(s["w_scale"].shape[1]):
+                w[j * 128:j * 128 + 128, k * 128:k * 128 + 128] *= s["w_scale"][k, j].double()
+        y = torch.mm(a, w.t().contiguous())
+        return y if s["bias"] is None else y + s["bias"].double()
+    return _exact_logits(s)
