@@ -149,7 +149,7 @@ def _quantized(x, block_rows):
     padded = torch.nn.functional.pad(x.float(), (0, nb * 128 - n, 0, rb * block_rows - rows)).view(rb, block_rows, nb, 128)
     amax = padded.abs().amax(dim=(1, 3))
     zero = amax < 2.0 ** -100
-    inv = torch.where(zero, 1.0, 448.0 / amax)
+    inv = torch.where(zero, 1.0, torch.full_like(amax, 448.0) / amax)  # (a number over a tensor would be its reciprocal, rounded, times the number)
     q = (padded * inv[:, None, :, None]).to(F8).view(rb * block_rows, nb * 128)[:rows, :n]
     return q.contiguous(), torch.where(zero, 1.0, amax / 448.0).t().contiguous()
 
