@@ -179,7 +179,8 @@ const char *gr4ad_strerror(int status);
 
 /* Message of the last failing call on this decoder ("" if none).  With
  * dec == NULL: the last failure on this thread of gr4ad_decode_init or of an
- * entry point that takes no decoder (gr4ad_op_select_static). */
+ * entry point that takes no decoder and says so (gr4ad_op_select_static, gr4ad_op_paged_attention, gr4ad_op_quantize_blocks,
+ * gr4ad_op_linear_fp8_block, gr4ad_op_adjust_logits). */
 const char *gr4ad_last_error(const gr4ad_decoder *dec);
 
 /*
@@ -273,6 +274,85 @@ int gr4ad_op_context_attention(gr4ad_dtype dtype, const void *q_dev, const void 
  * callers that keep a per-beam cache of their own.) */
 int gr4ad_op_gather_rows(gr4ad_dtype dtype, const void *src_dev, const int32_t *parent_dev, void *dst_dev, int32_t B, int32_t n,
                          int32_t k, int64_t row_elems, int64_t row_stride, void *hip_stream);
+
+/*
+ * gr4ad_op_paged_attention -- attention of new tokens over a paged cache of keys and values, for servers that keep what a user's sequence has computed
+ * between calls.  A batch of B sequences has N new tokens; those of sequence b are the rows q_start[b] .. q_start[b+1]-1 of q, and seq_len[b] is its
+ * length with them, so row i of its m_b rows stands at position p = seq_len[b] - m_b + i.  Any mix of single tokens, chunks of a prompt and sequences
+ * without a new token.  Row at p sees key j if 0 <= j <= p and, with a window > 0, also p - j < window or j < sinks (the first tokens stay visible):
+ *   out[row, h, :] = sum_j softmax_j(scale * q[row, h, :] . k_j) v_j,      heads h of one group of H / H_kv share key head h / (H / H_kv);
+ * a row that sees no key is zero.  Keys and values that a row does not see never reach it, whatever they hold.
+ *
+ *   cache          where keys and values live (the struct is host memory).  Position j of sequence b lies on page page_table[b, j / page_size], slot
+ *                  j % page_size.  Keys of a page are [H_kv, page_size, dh], values [H_kv, dh, page_size] (transposed).  Sequences may share pages.
+ *                  A page number outside [0, n_pages): the positions on it count as absent.
+ *   q              [N, H, dh] dtype, rows q_stride elements apart (a part of a wider row is fine)
+ *   k_new, v_new   [N, H_kv, dh] dtype, rows kv_stride elements apart: written into their pages first; both NULL if the pages hold them already.
+ *                  No two new tokens may lie on one slot of one page
+ *   q_start        [B+1] int32 device, ascending from >= 0 to <= N; rows in no sequence are left as they are.  seq_len [B] int32 device, at most
+ *                  max_pages * page_size (clamped).  Tokens at negative positions (seq_len[b] < m_b) are neither written nor see anything
+ *   out            [N, H, dh] dtype, dense
+ *   workspace_dev  gr4ad_op_paged_attention_workspace_bytes bytes of scratch (0: none), not shared by calls that overlap in time
+ * float32 sums, maxima and normalisers; bf16 weights of the softmax are rounded once, as operands of the product with the values.  Same bits from run
+ * to run; a row's bits may depend on the batch it is in (which decides how its keys are split).  head widths 16, 32, 64, 128; page_size a power of two
+ * from 16 to 1024; q, k_new and v_new with their rows, out, both page arrays and the workspace 16-byte aligned.
+ */
+typedef struct {
+    void *k_pages, *v_pages;         /* device, of the call's dtype */
+    const int32_t *page_table;       /* device [B, max_pages] */
+    int32_t n_pages, page_size, max_pages;
+    int32_t H_kv, dh;
+} gr4ad_paged_cache;
+size_t gr4ad_op_paged_attention_workspace_bytes(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, int32_t B, int32_t N, int32_t H, int32_t window, int32_t sinks);
+int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, const void *q_dev, int64_t q_stride, const void *k_new_dev, const void *v_new_dev,
+                             int64_t kv_stride, const int32_t *q_start_dev, const int32_t *seq_len_dev, void *out_dev, int32_t B, int32_t N, int32_t H, float scale,
+                             int32_t window, int32_t sinks, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * gr4ad_op_quantize_blocks -- FP8 operands with a scale for every block of 128 values of a row (block_rows = 1: activations) or of 128 x 128 values
+ * (block_rows = 128: weights), so that a column of large values costs its own block the resolution and no other:
+ *   scale = amax / 448 and q = nearest OCP E4M3 value (ties to even) of x * (448 / amax), amax the block's largest magnitude (float32 operations);
+ *   a block with amax < 2^-100 becomes zeros with scale 1.  A NaN becomes the E4M3 NaN; of a block that holds an infinity nothing is defined but that it has NaNs.
+ * x [rows, n] float32 or bf16, rows x_stride elements apart; q [rows, n] bytes; scale [ceil(n / 128), ceil(rows / block_rows)] float32: blocks along n
+ * first, as the product reads them.  Any rows and n >= 1; the last blocks may be partial.
+ */
+int gr4ad_op_quantize_blocks(gr4ad_dtype dtype, const void *x_dev, int64_t x_stride, void *q_dev, float *scale_dev, int32_t rows, int32_t n, int32_t block_rows,
+                             void *hip_stream);
+
+/*
+ * gr4ad_op_linear_fp8_block -- C[M,N] = sum_kb a_scale[kb, m] * w_scale[kb, n / 128] * (sum over the 128 k of block kb of Aq[m,k] Wq[n,k]) (+ bias[n])
+ * on operands of gr4ad_op_quantize_blocks (Aq with block_rows = 1, Wq with block_rows = 128): a_scale [ceil(K/128), M], w_scale [ceil(K/128), ceil(N/128)],
+ * bias [N] float32 or NULL.  Every block's product is scaled and added in float32.  C is bf16, or IEEE half with out_f16 != 0 (logits for
+ * gr4ad_op_adjust_logits_f16 and gr4ad_op_select_f16): the matrix cores keep about 16 bits of an FP8 product's sum, so there is no float32 form.
+ * Any M, N, K >= 1; rows dense.
+ */
+int gr4ad_op_linear_fp8_block(const void *Aq_dev, const float *a_scale_dev, const void *Wq_dev, const float *w_scale_dev, const float *bias_dev, void *C_dev,
+                              int32_t M, int32_t N, int32_t K, int32_t out_f16, void *hip_stream);
+
+/*
+ * gr4ad_op_adjust_logits -- penalties for repeated tokens, biases and grammar masks on rows of logits, in front of the selection.  With c the number of
+ * times token v occurs in the row's history, in float32 and in this order:
+ *   l = c > 0 ? (l > 0 ? l / repetition : l * repetition) : l;   l -= frequency * c + (c > 0 ? presence : 0);   l += bias[bias_row, v];
+ *   l = -inf where the row's mask forbids v (whatever the logit holds).
+ * logits, out [rows, V] float32 (_f16: IEEE half, rounded once), out may be logits itself.  Every rule is optional (NULL).  The struct is host memory,
+ * its pointers device memory.
+ */
+typedef struct {
+    const int32_t *history;      /* [rows, history_stride]: earlier tokens of each row, any order; entries outside [0, V) are passed over */
+    const int32_t *history_len;  /* [rows], clamped to [0, history_stride]; NULL = history_stride */
+    int32_t history_stride;
+    const float *repetition;     /* [rows] factors > 0 */
+    const float *presence;       /* [rows] */
+    const float *frequency;      /* [rows] */
+    const float *bias;           /* [n_bias, V] */
+    const int32_t *bias_row;     /* [rows]: row of bias, outside [0, n_bias) = none; NULL = row 0 for every row */
+    int32_t n_bias;
+    const uint32_t *mask;        /* [n_masks, ceil(V / 32)]: bit v % 32 of word v / 32 set = token v is allowed */
+    const int32_t *mask_row;     /* [rows]: row of mask, negative = none, >= n_masks = every token is forbidden; NULL = row 0 for every row */
+    int32_t n_masks;
+} gr4ad_logit_rules;
+int gr4ad_op_adjust_logits(const float *logits_dev, float *out_dev, int32_t rows, int32_t V, const gr4ad_logit_rules *rules, void *hip_stream);
+int gr4ad_op_adjust_logits_f16(const void *logits_f16_dev, void *out_f16_dev, int32_t rows, int32_t V, const gr4ad_logit_rules *rules, void *hip_stream);
 
 /*
  * Per-kernel timing for measurement (process-wide, off by default).  While on,

@@ -20,6 +20,8 @@ EXPORTS = ["gr4ad_decode_init", "gr4ad_decode_workspace_bytes", "gr4ad_decode_ba
            "gr4ad_decode_free", "gr4ad_strerror", "gr4ad_last_error", "gr4ad_op_linear", "gr4ad_op_select_workspace_bytes",
            "gr4ad_op_quantize_rows", "gr4ad_op_linear_fp8",
            "gr4ad_op_select", "gr4ad_op_select_f16", "gr4ad_op_select_static", "gr4ad_op_cross_attention_workspace_bytes", "gr4ad_op_cross_attention", "gr4ad_op_context_attention", "gr4ad_op_gather_rows",
+           "gr4ad_op_paged_attention_workspace_bytes", "gr4ad_op_paged_attention", "gr4ad_op_quantize_blocks", "gr4ad_op_linear_fp8_block",
+           "gr4ad_op_adjust_logits", "gr4ad_op_adjust_logits_f16",
            "gr4ad_profile_enable",
            "gr4ad_profile_kernel_count", "gr4ad_profile_kernel_name", "gr4ad_profile_read"]
 
@@ -52,6 +54,16 @@ class Weights(C.Structure):
 class TabsConfig(C.Structure):
     _fields_ = [("n_levels", C.c_int32), ("beam_base", _IP), ("max_beam", _IP), ("codebook", _IP), ("qps_peak", C.c_double),
                 ("scale_min", C.c_double), ("scale_max", C.c_double), ("step", C.c_double), ("tau_s", C.c_double)]
+
+
+class PagedCacheDesc(C.Structure):
+    _fields_ = [("k_pages", _VP), ("v_pages", _VP), ("page_table", _VP), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("max_pages", C.c_int32),
+                ("H_kv", C.c_int32), ("dh", C.c_int32)]
+
+
+class LogitRules(C.Structure):
+    _fields_ = [("history", _VP), ("history_len", _VP), ("history_stride", C.c_int32), ("repetition", _VP), ("presence", _VP), ("frequency", _VP),
+                ("bias", _VP), ("bias_row", _VP), ("n_bias", C.c_int32), ("mask", _VP), ("mask_row", _VP), ("n_masks", C.c_int32)]
 
 
 class Gr4adError(RuntimeError):
@@ -109,6 +121,18 @@ def lib():
         L.gr4ad_op_cross_attention_workspace_bytes.argtypes = [C.c_int, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
         L.gr4ad_op_gather_rows.restype = C.c_int
         L.gr4ad_op_gather_rows.argtypes = [C.c_int, _VP, _VP, _VP, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64, _VP]
+        L.gr4ad_op_paged_attention_workspace_bytes.restype = C.c_size_t
+        L.gr4ad_op_paged_attention_workspace_bytes.argtypes = [C.c_int, C.POINTER(PagedCacheDesc)] + [C.c_int32] * 5
+        L.gr4ad_op_paged_attention.restype = C.c_int
+        L.gr4ad_op_paged_attention.argtypes = [C.c_int, C.POINTER(PagedCacheDesc), _VP, C.c_int64, _VP, _VP, C.c_int64, _VP, _VP, _VP, C.c_int32, C.c_int32, C.c_int32,
+                                               C.c_float, C.c_int32, C.c_int32, _VP, C.c_size_t, _VP]
+        L.gr4ad_op_quantize_blocks.restype = C.c_int
+        L.gr4ad_op_quantize_blocks.argtypes = [C.c_int, _VP, C.c_int64, _VP, _VP, C.c_int32, C.c_int32, C.c_int32, _VP]
+        L.gr4ad_op_linear_fp8_block.restype = C.c_int
+        L.gr4ad_op_linear_fp8_block.argtypes = [_VP] * 6 + [C.c_int32] * 4 + [_VP]
+        for f in (L.gr4ad_op_adjust_logits, L.gr4ad_op_adjust_logits_f16):
+            f.restype = C.c_int
+            f.argtypes = [_VP, _VP, C.c_int32, C.c_int32, C.POINTER(LogitRules), _VP]
         L.gr4ad_profile_enable.restype = C.c_int
         L.gr4ad_profile_enable.argtypes = [C.c_int]
         L.gr4ad_profile_kernel_count.restype = C.c_int
@@ -385,6 +409,157 @@ def op_gather_rows(src, parent, k=None, row_elems=None, stream=None):
     _check(lib().gr4ad_op_gather_rows(dtype_code(src.dtype), src.data_ptr(), parent.data_ptr(), dst.data_ptr(), B, n, k,
                                       stride if row_elems is None else row_elems, stride, _stream_ptr(stream)))
     return dst
+
+
+# ---- an autoregressive step's operators: attention over pages, block-scaled FP8 products, logits in front of the selection
+# These check devices, types, shapes and strides before the library sees a pointer, launch on `stream` (default: the current one of the operands' device),
+# and hold what they allocate themselves for that stream.
+def _operands(what, first, *rest):
+    """ValueError unless every tensor (None is passed over) lies on the GPU of `first`."""
+    dev = first.device
+    if dev.type != "cuda":
+        raise ValueError("%s: tensors on the GPU are needed, got %s" % (what, dev))
+    for t in rest:
+        if t is not None and t.device != dev:
+            raise ValueError("%s: tensors on %s and %s" % (what, dev, t.device))
+
+
+def _typed(what, t, dtype, shape):
+    """ValueError unless t (None is passed over) is dense, of the type and of the shape (None: any size)."""
+    if t is None:
+        return
+    if t.dtype != dtype or t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)) or not t.is_contiguous():
+        raise ValueError("%s: needs a dense %s tensor of shape %s, got %s %s%s" % (what, dtype, tuple(shape), t.dtype, tuple(t.shape),
+                                                                                   "" if t.is_contiguous() else " (strided)"))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+class _On:
+    """The device and stream of a call: what is allocated and launched inside belongs to them."""
+
+    def __init__(self, device, stream):
+        self.device = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+        self.given = stream
+
+    def __enter__(self):
+        if self.device:
+            self.device.__enter__()
+        self.stream = torch.cuda.stream(self.given) if self.given is not None else None
+        if self.stream:
+            self.stream.__enter__()
+        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+    def __exit__(self, *e):
+        if self.stream:
+            self.stream.__exit__(*e)
+        if self.device:
+            self.device.__exit__(*e)
+
+
+def op_paged_attention(q, k_pages, v_pages, page_table, q_start, seq_len, k_new=None, v_new=None, scale=None, window=0, sinks=0, out=None, workspace=None, stream=None):
+    """gr4ad_op_paged_attention: q [N,H,dh] (rows may be strided), k_pages [n_pages,H_kv,page_size,dh], v_pages [n_pages,H_kv,dh,page_size], page_table
+    [B,max_pages], q_start [B+1], seq_len [B] int32; k_new, v_new [N,H_kv,dh] are written into their pages first.  scale: 1/sqrt(dh) if None."""
+    what = "op_paged_attention"
+    _operands(what, q, k_pages, v_pages, page_table, q_start, seq_len, k_new, v_new, out, workspace)
+    if q.dtype not in (torch.float32, torch.bfloat16) or q.dim() != 3 or k_pages.dim() != 4 or page_table.dim() != 2:
+        raise ValueError("%s: q [N,H,dh] float32 or bfloat16, k_pages [n_pages,H_kv,page_size,dh], page_table [B,max_pages]" % what)
+    N, H, dh = q.shape
+    n_pages, H_kv, page, _ = k_pages.shape
+    B, max_pages = page_table.shape
+    _typed(what + " k_pages", k_pages, q.dtype, (None, None, None, dh))
+    _typed(what + " v_pages", v_pages, q.dtype, (n_pages, H_kv, dh, page))
+    _typed(what + " page_table", page_table, torch.int32, (None, None))
+    _typed(what + " q_start", q_start, torch.int32, (B + 1,))
+    _typed(what + " seq_len", seq_len, torch.int32, (B,))
+    _typed(what + " out", out, q.dtype, (N, H, dh))
+    for name, t, heads in (("q", q, H), ("k_new", k_new, H_kv), ("v_new", v_new, H_kv)):
+        if t is not None and (t.dtype != q.dtype or tuple(t.shape) != (N, heads, dh) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dh)):
+            raise ValueError("%s: %s must be %s [%d,%d,%d] with dense rows, got %s %s strides %s" % (what, name, q.dtype, N, heads, dh, t.dtype, tuple(t.shape), t.stride()))
+    row = lambda t, heads: t.stride(0) if N > 1 else heads * dh  # noqa: E731
+    kv_stride = 0 if k_new is None else row(k_new, H_kv)
+    if k_new is not None and v_new is not None and row(v_new, H_kv) != kv_stride:
+        raise ValueError("%s: rows of k_new and v_new lie %d and %d values apart" % (what, kv_stride, row(v_new, H_kv)))
+    L = lib()
+    cache = PagedCacheDesc(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), n_pages, page, max_pages, H_kv, dh)
+    dt = dtype_code(q.dtype)
+    with _On(q.device, stream) as st:
+        if out is None:
+            out = torch.empty(N, H, dh, dtype=q.dtype, device=q.device)
+        if workspace is None:
+            need = int(L.gr4ad_op_paged_attention_workspace_bytes(dt, C.byref(cache), B, N, H, window, sinks))
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        _check(L.gr4ad_op_paged_attention(dt, C.byref(cache), q.data_ptr(), row(q, H), _ptr(k_new), _ptr(v_new), kv_stride, q_start.data_ptr(), seq_len.data_ptr(),
+                                          out.data_ptr(), B, N, H, dh ** -0.5 if scale is None else scale, window, sinks, _ptr(workspace),
+                                          workspace.numel() * workspace.element_size() if workspace is not None else 0, st))
+    return out
+
+
+def op_quantize_blocks(x, block_rows=1, stream=None):
+    """x [rows, n] float32 or bf16 (rows may be strided) -> (q [rows, n] uint8 holding E4M3 bytes, scale [ceil(n/128), ceil(rows/block_rows)] float32)."""
+    _operands("op_quantize_blocks", x)
+    if x.dtype not in (torch.float32, torch.bfloat16) or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1) or block_rows not in (1, 128):
+        raise ValueError("op_quantize_blocks: x [rows, n] float32 or bfloat16 with dense rows, block_rows 1 or 128; got %s %s strides %s, %r" % (x.dtype, tuple(x.shape), x.stride(), block_rows))
+    rows, n = x.shape
+    with _On(x.device, stream) as st:
+        q = torch.empty(rows, n, dtype=torch.uint8, device=x.device)
+        scale = torch.empty(-(-n // 128), -(-rows // block_rows), dtype=torch.float32, device=x.device)
+        _check(lib().gr4ad_op_quantize_blocks(dtype_code(x.dtype), x.data_ptr(), x.stride(0) if rows > 1 else n, q.data_ptr(), scale.data_ptr(), rows, n, block_rows, st))
+    return q, scale
+
+
+def op_linear_fp8_block(Aq, a_scale, Wq, w_scale, bias=None, out_dtype=torch.bfloat16, out=None, stream=None):
+    """gr4ad_op_linear_fp8_block on the outputs of op_quantize_blocks (block_rows 1 for Aq [M,K], 128 for Wq [N,K]); out_dtype bfloat16 or float16."""
+    what = "op_linear_fp8_block"
+    _operands(what, Aq, a_scale, Wq, w_scale, bias, out)
+    if out_dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("%s: out_dtype bfloat16 or float16, got %s" % (what, out_dtype))
+    _typed(what + " Aq", Aq, torch.uint8, (None, None))
+    M, K = Aq.shape
+    _typed(what + " Wq", Wq, torch.uint8, (None, K))
+    N = Wq.shape[0]
+    _typed(what + " a_scale", a_scale, torch.float32, (-(-K // 128), M))
+    _typed(what + " w_scale", w_scale, torch.float32, (-(-K // 128), -(-N // 128)))
+    _typed(what + " bias", bias, torch.float32, (N,))
+    _typed(what + " out", out, out_dtype, (M, N))
+    with _On(Aq.device, stream) as st:
+        if out is None:
+            out = torch.empty(M, N, dtype=out_dtype, device=Aq.device)
+        _check(lib().gr4ad_op_linear_fp8_block(Aq.data_ptr(), a_scale.data_ptr(), Wq.data_ptr(), w_scale.data_ptr(), _ptr(bias), out.data_ptr(), M, N, K,
+                                               int(out_dtype == torch.float16), st))
+    return out
+
+
+def op_adjust_logits(logits, history=None, history_len=None, repetition=None, presence=None, frequency=None, bias=None, bias_row=None, mask=None, mask_row=None,
+                     out=None, stream=None):
+    """gr4ad_op_adjust_logits (float32) or gr4ad_op_adjust_logits_f16 (float16): logits [..., V] -> the same shape; out may be logits.
+    history [rows, most] int32, history_len / bias_row / mask_row [rows] int32, repetition / presence / frequency [rows] float32, bias [n, V] float32,
+    mask [n, ceil(V/32)] int32 (bit v % 32 of word v // 32 set: token v is allowed)."""
+    what = "op_adjust_logits"
+    _operands(what, logits, history, history_len, repetition, presence, frequency, bias, bias_row, mask, mask_row, out)
+    if logits.dtype not in (torch.float32, torch.float16) or logits.dim() < 1 or not logits.is_contiguous():
+        raise ValueError("%s: dense float32 or float16 logits [..., V], got %s %s" % (what, logits.dtype, tuple(logits.shape)))
+    V = logits.shape[-1]
+    rows = logits.numel() // V if V else 0
+    _typed(what + " out", out, logits.dtype, logits.shape)
+    _typed(what + " history", history, torch.int32, (rows, None))
+    _typed(what + " bias", bias, torch.float32, (None, V))
+    _typed(what + " mask", mask, torch.int32, (None, -(-V // 32)))
+    for name, t, dt in (("history_len", history_len, torch.int32), ("bias_row", bias_row, torch.int32), ("mask_row", mask_row, torch.int32),
+                        ("repetition", repetition, torch.float32), ("presence", presence, torch.float32), ("frequency", frequency, torch.float32)):
+        if t is not None:
+            _typed("%s %s" % (what, name), t, dt, (rows,))
+    L = lib()
+    rules = LogitRules(_ptr(history), _ptr(history_len), 0 if history is None else history.shape[1], _ptr(repetition), _ptr(presence), _ptr(frequency),
+                       _ptr(bias), _ptr(bias_row), 0 if bias is None else bias.shape[0], _ptr(mask), _ptr(mask_row), 0 if mask is None else mask.shape[0])
+    entry = L.gr4ad_op_adjust_logits if logits.dtype == torch.float32 else L.gr4ad_op_adjust_logits_f16
+    with _On(logits.device, stream) as st:
+        if out is None:
+            out = torch.empty_like(logits)
+        _check(entry(logits.data_ptr(), out.data_ptr(), rows, V, C.byref(rules), st))
+    return out
 
 
 # ---- host-side serving policies (include/gr4ad_serving.h) ------------------------------

@@ -1,0 +1,318 @@
+// FP8 (OCP E4M3) operands with a scale for every block of 128 values along the contraction, and their product:
+//     C[m, n] = sum_kb sa[kb, m] sw[kb, n / 128] sum_{k in block kb} Aq[m, k] Wq[n, k]  (+ bias[n]).
+//
+//  * quantize_blocks<..>   1 x 128 or 128 x 128 blocks, one pass over the values.
+//  * gemm_block_few<MG>    up to 64 rows: the weights stream from memory to the matrix cores' operands, wavefronts split K.
+//  * gemm_block_tile<..>   tiles of C, operands staged in LDS.
+//
+// v_mfma_f32_16x16x128_f8f6f4 contracts exactly one block, so a block's product leaves it as 16 x 16 sums that one multiply-add each scales into the
+// float32 accumulators.  The weights are the first operand: a lane then owns one row of A, whose scale is one register, and four consecutive columns of C.
+#include "common.h"
+
+namespace {
+
+typedef int intx8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ uint2 e4m3x8(const float (&v)[8], float f) {
+    int w0 = 0, w1 = 0;
+    w0 = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * f, v[1] * f, w0, false);
+    w0 = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * f, v[3] * f, w0, true);
+    w1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[4] * f, v[5] * f, w1, false);
+    w1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * f, v[7] * f, w1, true);
+    return make_uint2((unsigned)w0, (unsigned)w1);
+}
+
+__device__ __forceinline__ float row16_max(float v) {  // over the 16 lanes of a row
+    v = fmaxf(v, dpp_move<0x128, 0xF>(v, v));
+    v = fmaxf(v, dpp_move<0x124, 0xF>(v, v));
+    v = fmaxf(v, dpp_move<0x122, 0xF>(v, v));
+    return fmaxf(v, dpp_move<0x121, 0xF>(v, v));
+}
+
+struct BlockScale {
+    float scale, inv;
+    __device__ __forceinline__ explicit BlockScale(float amax) {
+        const bool zero = amax < 0x1p-100f;
+        scale = zero ? 1.0f : amax / 448.0f;
+        inv = zero ? 1.0f : 448.0f / amax;
+    }
+};
+
+// Sixteen lanes hold a row's block, eight values each.  TALL: a workgroup owns one block of 128 x 128 (16 rows at a time, 8 times); otherwise 16 rows
+// by STEPS blocks, all of whose values are requested at once.
+template <typename T, bool TALL> __global__ __launch_bounds__(256) void quantize_blocks(const T *__restrict__ x, int64_t ldx, uint8_t *__restrict__ q, float *__restrict__ scale, int rows,
+                                                                                        int n, int nb, int bands) {
+    constexpr int STEPS = TALL ? 8 : sizeof(T) == 2 ? 4 : 2;
+    const int band = blockIdx.x % bands, kb0 = blockIdx.x / bands * (TALL ? 1 : STEPS), lane16 = threadIdx.x % 16, r16 = threadIdx.x / 16;
+    float v[STEPS][8], amax[STEPS];
+    auto row_of = [&](int i) { return TALL ? band * 128 + i * 16 + r16 : band * 16 + r16; };
+    auto col_of = [&](int i) { return (TALL ? kb0 : kb0 + i) * 128 + lane16 * 8; };
+#pragma unroll
+    for (int i = 0; i < STEPS; i++) {
+        const int r = row_of(i), c = col_of(i);
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[i][e] = 0.0f;
+        if (r < rows && c < n) {
+            const T *src = x + (int64_t)r * ldx + c;
+            if (c + 8 <= n) {  // (rows may start anywhere)
+                T t[8];
+                __builtin_memcpy(t, src, 8 * sizeof(T));
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[i][e] = to_f(t[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if (c + e < n) v[i][e] = to_f(src[e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < STEPS; i++) {
+        amax[i] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; e++) amax[i] = fmaxf(amax[i], fabsf(v[i][e]));
+    }
+    if (TALL) {
+        __shared__ float part[4];
+        float m = amax[0];
+#pragma unroll
+        for (int i = 1; i < STEPS; i++) m = fmaxf(m, amax[i]);
+        m = wave_max(m);
+        if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = m;
+        __syncthreads();
+        m = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+#pragma unroll
+        for (int i = 0; i < STEPS; i++) amax[i] = m;
+        if (threadIdx.x == 0) scale[(int64_t)kb0 * bands + band] = BlockScale(m).scale;
+    }
+#pragma unroll
+    for (int i = 0; i < STEPS; i++) {
+        const BlockScale s(TALL ? amax[i] : row16_max(amax[i]));
+        const int r = row_of(i), c = col_of(i);
+        if (r >= rows || c >= n) continue;
+        if (!TALL && lane16 == 0) scale[(int64_t)(kb0 + i) * rows + r] = s.scale;
+        const uint2 w = e4m3x8(v[i], s.inv);
+        uint8_t *dst = q + (int64_t)r * n + c;
+        if (c + 8 <= n) {
+            __builtin_memcpy(dst, &w, 8);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (c + e < n) dst[e] = (uint8_t)((e < 4 ? w.x : w.y) >> (8 * (e % 4)));
+        }
+    }
+}
+
+// 16 bytes at column k of a row of K bytes, zeros past its end; rows may start anywhere
+__device__ __forceinline__ intx4 bytes16(const uint8_t *row, int k, int K) {
+    intx4 r = {0, 0, 0, 0};
+    if (k + 16 <= K) {
+        __builtin_memcpy(&r, row + k, 16);
+    } else {
+        for (int i = 0; i < 16 && k + i < K; i++) r[i / 4] |= (int)row[k + i] << (8 * (i % 4));
+    }
+    return r;
+}
+__device__ __forceinline__ intx8 join8(intx4 lo, intx4 hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
+__device__ __forceinline__ floatx4 mfma_block(intx8 w, intx8 a) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a, floatx4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0, 0, 0, 0);
+}
+
+struct BlockGemm {
+    const uint8_t *A, *W;
+    const float *sa, *sw, *bias;
+    void *C;
+    int M, N, K, nb, wb;  // blocks along K, and along N
+    int out_f16;
+};
+
+// four consecutive columns of one row of C
+__device__ __forceinline__ void store4(const BlockGemm &g, int m, int n, floatx4 v) {
+    if (m >= g.M) return;
+    uint16_t h[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const float x = v[e] + (g.bias && n + e < g.N ? g.bias[n + e] : 0.0f);
+        if (g.out_f16) {
+            const _Float16 y = (_Float16)x;
+            __builtin_memcpy(&h[e], &y, 2);
+        } else {
+            const bf16 y = (bf16)x;
+            __builtin_memcpy(&h[e], &y, 2);
+        }
+    }
+    uint16_t *dst = (uint16_t *)g.C + (int64_t)m * g.N + n;
+    if (n + 4 <= g.N) {
+        __builtin_memcpy(dst, h, 8);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (n + e < g.N) dst[e] = h[e];
+    }
+}
+
+// Up to 16 MG rows: 16 columns of C per workgroup, whose 8 wavefronts take blocks of K in turn and are joined in LDS in their order.
+template <int MG> __global__ __launch_bounds__(512) void gemm_block_few(BlockGemm g) {
+    constexpr int NW = 8;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, c = lane / 16, n0 = blockIdx.x * 16;
+    const uint8_t *w = g.W + (int64_t)min(n0 + r, g.N - 1) * g.K;
+    const uint8_t *a[MG];
+    int m[MG];
+#pragma unroll
+    for (int i = 0; i < MG; i++) {
+        m[i] = min(16 * i + r, g.M - 1);
+        a[i] = g.A + (int64_t)m[i] * g.K;
+    }
+    floatx4 acc[MG];
+#pragma unroll
+    for (int i = 0; i < MG; i++) acc[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int kb = wave; kb < g.nb; kb += NW) {
+        const int k = kb * 128 + 32 * c;
+        const intx8 wf = join8(bytes16(w, k, g.K), bytes16(w, k + 16, g.K));
+        const float sw = g.sw[(int64_t)kb * g.wb + n0 / 128];
+#pragma unroll
+        for (int i = 0; i < MG; i++) {
+            const floatx4 p = mfma_block(wf, join8(bytes16(a[i], k, g.K), bytes16(a[i], k + 16, g.K)));
+            const float s = g.sa[(int64_t)kb * g.M + m[i]] * sw;
+#pragma unroll
+            for (int v = 0; v < 4; v++) acc[i][v] = fmaf(p[v], s, acc[i][v]);
+        }
+    }
+    __shared__ floatx4 part[NW][MG][64];
+#pragma unroll
+    for (int i = 0; i < MG; i++) part[wave][i][lane] = acc[i];
+    __syncthreads();
+    if (wave < MG) {
+        floatx4 s = part[0][wave][lane];
+#pragma unroll
+        for (int x = 1; x < NW; x++) s += part[x][wave][lane];
+        store4(g, 16 * wave + r, n0 + 4 * c, s);
+    }
+}
+
+// TM x TN tiles of C on four wavefronts (2 x 2).  The next block's operands travel to registers while this one's multiply.  A tile row is one block, 128
+// bytes; its 16-byte chunk p lies at p ^ (row / 2 % 8).
+template <int TM, int TN> __global__ __launch_bounds__(256) void gemm_block_tile(BlockGemm g) {
+    constexpr int WM = TM / 2, WN = TN / 2, GM = WM / 16, GN = WN / 16, LA = TM * 8 / 256, LW = TN * 8 / 256;
+    __shared__ intx4 sA[TM * 8], sW[TN * 8];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, c = lane / 16;
+    const int wm = wave / 2, wn = wave % 2, tiles_m = (g.M + TM - 1) / TM;
+    const int m0 = (int)(blockIdx.x % tiles_m) * TM, n0 = (int)(blockIdx.x / tiles_m) * TN;
+    intx4 ra[LA], rw[LW];
+    auto load = [&](int kb) {
+#pragma unroll
+        for (int i = 0; i < LA; i++) {
+            const int id = i * 256 + threadIdx.x;
+            ra[i] = bytes16(g.A + (int64_t)min(m0 + id / 8, g.M - 1) * g.K, kb * 128 + id % 8 * 16, g.K);
+        }
+#pragma unroll
+        for (int i = 0; i < LW; i++) {
+            const int id = i * 256 + threadIdx.x;
+            rw[i] = bytes16(g.W + (int64_t)min(n0 + id / 8, g.N - 1) * g.K, kb * 128 + id % 8 * 16, g.K);
+        }
+    };
+    auto slot = [](int row, int p) { return row * 8 + (p ^ ((row >> 1) & 7)); };
+    floatx4 acc[GM][GN];
+#pragma unroll
+    for (int i = 0; i < GM; i++)
+#pragma unroll
+        for (int j = 0; j < GN; j++) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    load(0);
+    for (int kb = 0; kb < g.nb; kb++) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < LA; i++) {
+            const int id = i * 256 + threadIdx.x;
+            sA[slot(id / 8, id % 8)] = ra[i];
+        }
+#pragma unroll
+        for (int i = 0; i < LW; i++) {
+            const int id = i * 256 + threadIdx.x;
+            sW[slot(id / 8, id % 8)] = rw[i];
+        }
+        __syncthreads();
+        if (kb + 1 < g.nb) load(kb + 1);
+        const float sw = g.sw[(int64_t)kb * g.wb + (n0 + wn * WN) / 128];
+        intx8 wf[GN];
+#pragma unroll
+        for (int j = 0; j < GN; j++) {
+            const int row = wn * WN + 16 * j + r;
+            wf[j] = join8(sW[slot(row, c)], sW[slot(row, c + 4)]);
+        }
+#pragma unroll
+        for (int i = 0; i < GM; i++) {
+            const int row = wm * WM + 16 * i + r;
+            const intx8 af = join8(sA[slot(row, c)], sA[slot(row, c + 4)]);
+            const float s = g.sa[(int64_t)kb * g.M + min(m0 + row, g.M - 1)] * sw;
+#pragma unroll
+            for (int j = 0; j < GN; j++) {
+                const floatx4 p = mfma_block(wf[j], af);
+#pragma unroll
+                for (int v = 0; v < 4; v++) acc[i][j][v] = fmaf(p[v], s, acc[i][j][v]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < GM; i++)
+#pragma unroll
+        for (int j = 0; j < GN; j++) store4(g, m0 + wm * WM + 16 * i + r, n0 + wn * WN + 16 * j + 4 * c, acc[i][j]);
+}
+
+template <int TM, int TN> int launch_tile(const BlockGemm &g, hipStream_t st) {
+    const int64_t grid = ceil_div64(g.M, TM) * ceil_div64(g.N, TN);
+    if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
+    hipLaunchKernelGGL((gemm_block_tile<TM, TN>), dim3((unsigned)grid), dim3(256), 0, st, g);
+    GR4AD_LAUNCH_CHECK();
+    return GR4AD_OK;
+}
+
+int launch_block_gemm(const BlockGemm &g, hipStream_t st) {
+    ProfScope ps(KC_GEMM_F8_BLOCK, st, 2.0 * (double)g.M * g.N * g.K, ((double)g.M + g.N) * g.K + 2.0 * (double)g.M * g.N);
+    if (g.M <= 64) {
+        const unsigned grid = (unsigned)((g.N + 15) / 16);
+        if (g.M <= 16) hipLaunchKernelGGL(gemm_block_few<1>, dim3(grid), dim3(512), 0, st, g);
+        else if (g.M <= 32) hipLaunchKernelGGL(gemm_block_few<2>, dim3(grid), dim3(512), 0, st, g);
+        else hipLaunchKernelGGL(gemm_block_few<4>, dim3(grid), dim3(512), 0, st, g);
+        GR4AD_LAUNCH_CHECK();
+        return GR4AD_OK;
+    }
+    if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) < 256) return launch_tile<64, 64>(g, st);
+    return launch_tile<128, 128>(g, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int gr4ad_op_quantize_blocks(gr4ad_dtype dtype, const void *x, int64_t x_stride, void *q, float *scale, int32_t rows, int32_t n, int32_t block_rows, void *hip_stream) {
+    if (!x || !q || !scale) return gr4ad_set_thread_error(GR4AD_EINVAL, "quantize_blocks: NULL pointer");
+    if (dtype != GR4AD_F32 && dtype != GR4AD_BF16) return gr4ad_set_thread_error(GR4AD_EINVAL, "quantize_blocks: dtype %d", (int)dtype);
+    if (rows < 1 || n < 1 || x_stride < n) return gr4ad_set_thread_error(GR4AD_EINVAL, "quantize_blocks: %d rows of %d values, %lld apart", rows, n, (long long)x_stride);
+    if (block_rows != 1 && block_rows != 128) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "quantize_blocks: block_rows %d (1 or 128)", block_rows);
+    const size_t e = dtype == GR4AD_BF16 ? 2 : 4;
+    if ((uintptr_t)x % e || (uintptr_t)scale % 4) return gr4ad_set_thread_error(GR4AD_EINVAL, "quantize_blocks: misaligned pointer");
+    const bool tall = block_rows == 128;
+    const int64_t nb = ceil_div64(n, 128), bands = ceil_div64(rows, tall ? 128 : 16), steps = tall ? 1 : e == 2 ? 4 : 2, grid = bands * ceil_div64(nb, steps);
+    if (grid > 0x7fffffffLL) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "quantize_blocks: %d rows of %d values", rows, n);
+    hipStream_t st = (hipStream_t)hip_stream;
+    ProfScope ps(KC_QUANTIZE_BLOCKS, st, 0.0, (double)rows * n * (e + 1));
+#define QUANTIZE_(T, TALL) hipLaunchKernelGGL((quantize_blocks<T, TALL>), dim3((unsigned)grid), dim3(256), 0, st, (const T *)x, x_stride, (uint8_t *)q, scale, rows, n, (int)nb, (int)bands)
+    if (dtype == GR4AD_BF16) { if (tall) QUANTIZE_(bf16, true); else QUANTIZE_(bf16, false); }
+    else if (tall) QUANTIZE_(float, true);
+    else QUANTIZE_(float, false);
+#undef QUANTIZE_
+    GR4AD_LAUNCH_CHECK();
+    return GR4AD_OK;
+}
+
+int gr4ad_op_linear_fp8_block(const void *Aq, const float *a_scale, const void *Wq, const float *w_scale, const float *bias, void *C, int32_t M, int32_t N, int32_t K, int32_t out_f16,
+                              void *hip_stream) {
+    if (!Aq || !a_scale || !Wq || !w_scale || !C) return gr4ad_set_thread_error(GR4AD_EINVAL, "linear_fp8_block: NULL pointer");
+    if (M < 1 || N < 1 || K < 1) return gr4ad_set_thread_error(GR4AD_EINVAL, "linear_fp8_block: sizes %d x %d x %d must be positive", M, N, K);
+    if (M > 0x7fffff00 || N > 0x7fffff00 || K > 0x7fffff00) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "linear_fp8_block: sizes %d x %d x %d", M, N, K);
+    if ((uintptr_t)C % 2 || (uintptr_t)a_scale % 4 || (uintptr_t)w_scale % 4 || (uintptr_t)bias % 4) return gr4ad_set_thread_error(GR4AD_EINVAL, "linear_fp8_block: misaligned pointer");
+    BlockGemm g = {(const uint8_t *)Aq, (const uint8_t *)Wq, a_scale, w_scale, bias, C, M, N, K, (K + 127) / 128, (N + 127) / 128, out_f16 ? 1 : 0};
+    return launch_block_gemm(g, (hipStream_t)hip_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,140 @@
+// Penalties for repeated tokens, biases and grammar masks on rows of logits, in front of the selection.
+//
+//     l = c > 0 ? (l > 0 ? l / repetition : l * repetition) : l;  l -= frequency c + (c > 0 ? presence : 0);  l += bias;  forbidden: -inf
+//
+// c: how often the token occurs in the row's history.  One pass over the logits: a workgroup owns a stretch of one row, whose tokens it counts in LDS
+// (integer additions, so their order changes nothing) while the stretch's logits are on their way.
+#include "common.h"
+
+namespace {
+
+struct LogitArgs {
+    const void *in;
+    void *out;
+    int rows, V;
+    gr4ad_logit_rules r;
+};
+
+// 16 bytes of a row that may start anywhere (rows of V elements: a row's start is as aligned as V is)
+template <typename T> struct Piece {
+    static constexpr int N = 16 / sizeof(T);
+    T v[N];
+    __device__ __forceinline__ void load(const T *p) { __builtin_memcpy(v, p, 16); }
+    __device__ __forceinline__ void store(T *p) const { __builtin_memcpy(p, v, 16); }
+};
+
+// PIECES 16-byte pieces per thread
+template <typename T, int PIECES> __global__ __launch_bounds__(256) void adjust_logits(LogitArgs a, int stretches) {
+    constexpr int E = Piece<T>::N;
+    extern __shared__ unsigned count[];
+    const int span = blockDim.x * E * PIECES, row = blockIdx.x / stretches, v0 = (blockIdx.x - row * stretches) * span, V = a.V;
+    const gr4ad_logit_rules &r = a.r;
+    const int64_t at = (int64_t)row * V;
+    const T *in = (const T *)a.in + at;
+    T *out = (T *)a.out + at;
+    Piece<T> x[PIECES];
+    auto first = [&](int i) { return v0 + (i * (int)blockDim.x + (int)threadIdx.x) * E; };
+#pragma unroll
+    for (int i = 0; i < PIECES; i++) {
+        const int v = first(i);
+        if (v + E <= V) x[i].load(in + v);
+        else
+#pragma unroll
+            for (int e = 0; e < E; e++) x[i].v[e] = v + e < V ? in[v + e] : (T)0.0f;
+    }
+    int len = 0;
+    if (r.history) {
+        len = r.history_len ? r.history_len[row] : r.history_stride;
+        len = len < 0 ? 0 : len > r.history_stride ? r.history_stride : len;
+    }
+    if (len > 0) {
+        for (int i = threadIdx.x; i < span; i += blockDim.x) count[i] = 0;
+        __syncthreads();
+        const int32_t *h = r.history + (int64_t)row * r.history_stride;
+        for (int i = threadIdx.x; i < len; i += blockDim.x) {
+            const unsigned v = (unsigned)h[i] - (unsigned)v0;
+            if (v < (unsigned)span && h[i] < V) atomicAdd(&count[v], 1u);
+        }
+        __syncthreads();
+    }
+    const float rep = len > 0 && r.repetition ? r.repetition[row] : 1.0f, pres = len > 0 && r.presence ? r.presence[row] : 0.0f,
+                freq = len > 0 && r.frequency ? r.frequency[row] : 0.0f;
+    const float *bias = nullptr;
+    if (r.bias) {
+        const int b = r.bias_row ? r.bias_row[row] : 0;
+        if (b >= 0 && b < r.n_bias) bias = r.bias + (int64_t)b * V;
+    }
+    const uint32_t *mask = nullptr;
+    bool nothing = false;
+    if (r.mask) {
+        const int m = r.mask_row ? r.mask_row[row] : 0;
+        if (m >= r.n_masks) nothing = true;
+        else if (m >= 0) mask = r.mask + (int64_t)m * ((V + 31) / 32);
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; i++) {
+        const int v = first(i);
+        if (v >= V) continue;
+        unsigned allowed = nothing ? 0u : ~0u;
+        if (mask) allowed = mask[v / 32] >> (v % 32);
+        float b[E] = {};
+        if (bias) {
+            if (v + E <= V) __builtin_memcpy(b, bias + v, E * 4);
+            else
+#pragma unroll
+                for (int e = 0; e < E; e++) b[e] = v + e < V ? bias[v + e] : 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            float l = (float)x[i].v[e];
+            if (len > 0) {
+                const unsigned c = count[v - v0 + e];
+                if (c) {
+                    if (r.repetition) l = l > 0.0f ? l / rep : l * rep;
+                    l -= freq * (float)c + pres;
+                }
+            }
+            if (bias) l += b[e];
+            x[i].v[e] = (T)((allowed >> e & 1) ? l : -INFINITY);
+        }
+        if (v + E <= V) x[i].store(out + v);
+        else
+#pragma unroll
+            for (int e = 0; e < E; e++)
+                if (v + e < V) out[v + e] = x[i].v[e];
+    }
+}
+
+template <typename T> int adjust(const T *in, T *out, int32_t rows, int32_t V, const gr4ad_logit_rules *r, void *stream) {
+    if (!in || !out || !r) return gr4ad_set_thread_error(GR4AD_EINVAL, "adjust_logits: NULL pointer");
+    if (rows < 1 || V < 1) return gr4ad_set_thread_error(GR4AD_EINVAL, "adjust_logits: rows %d and V %d must be positive", rows, V);
+    if ((uintptr_t)in % sizeof(T) || (uintptr_t)out % sizeof(T)) return gr4ad_set_thread_error(GR4AD_EINVAL, "adjust_logits: misaligned logits");
+    if (r->history && r->history_stride < 1) return gr4ad_set_thread_error(GR4AD_EINVAL, "adjust_logits: history_stride %d must be positive", r->history_stride);
+    if (!r->history && (r->repetition || r->presence || r->frequency)) return gr4ad_set_thread_error(GR4AD_EINVAL, "adjust_logits: penalties without a history");
+    if (r->bias && r->n_bias < 1) return gr4ad_set_thread_error(GR4AD_EINVAL, "adjust_logits: n_bias %d must be positive", r->n_bias);
+    if (r->mask && r->n_masks < 1) return gr4ad_set_thread_error(GR4AD_EINVAL, "adjust_logits: n_masks %d must be positive", r->n_masks);
+    constexpr int E = Piece<T>::N, PIECES = 2;
+    const int threads = V <= 64 * E * PIECES ? 64 : V <= 128 * E * PIECES ? 128 : 256, span = threads * E * PIECES;
+    const int64_t stretches = ceil_div64(V, span), grid = rows * stretches;
+    if (grid > 0x7fffffffLL) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "adjust_logits: %d rows of %d logits", rows, V);
+    hipStream_t st = (hipStream_t)stream;
+    ProfScope ps(KC_ADJUST_LOGITS, st, 0.0, 2.0 * sizeof(T) * rows * (double)V);
+    LogitArgs a = {in, out, rows, V, *r};
+    hipLaunchKernelGGL((adjust_logits<T, PIECES>), dim3((unsigned)grid), dim3(threads), r->history ? span * sizeof(unsigned) : 0, st, a, (int)stretches);
+    GR4AD_LAUNCH_CHECK();
+    return GR4AD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gr4ad_op_adjust_logits(const float *logits, float *out, int32_t rows, int32_t V, const gr4ad_logit_rules *rules, void *hip_stream) {
+    return adjust<float>(logits, out, rows, V, rules, hip_stream);
+}
+
+int gr4ad_op_adjust_logits_f16(const void *logits, void *out, int32_t rows, int32_t V, const gr4ad_logit_rules *rules, void *hip_stream) {
+    return adjust<_Float16>((const _Float16 *)logits, (_Float16 *)out, rows, V, rules, hip_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,580 @@
+// Attention of new tokens over a paged cache of keys and values, with the cache's update.
+//
+// Sequence b has m_b new tokens, rows q_start[b] .. q_start[b+1]-1 of q, and len_b tokens with them; its row i stands at position
+// p = len_b - m_b + i and sees key j if 0 <= j <= p and (no window, or p - j < window, or j < sinks):
+//     out[row, h, :] = sum_j softmax_j(scale * q[row, h, :] . k_j) v_j,        keys and values of head h / (H / H_kv).
+//
+// The cache: keys [page][H_kv][slot][dh], values transposed [page][H_kv][dh][slot], so that a page of one head is one stretch of memory
+// and both operands of the two products, S^T = K Q^T and O^T = V^T P^T, are read along their contraction in 16-byte pieces.
+//
+//  * paged_append<T>        new keys and values into their pages.
+//  * paged_rows<T, DH>      16 rows (token, head of the group) of one (sequence, key head) per workgroup, whose wavefronts walk
+//                           stretches of the keys of their own; operands go from memory to registers.
+//  * paged_join<T, DH>      joins the stretches of several workgroups.
+#include "common.h"
+
+namespace {
+
+constexpr int kRows = 16;       // rows of a tile
+constexpr int kAppendKeys = 64; // positions of a tile of the update
+
+struct PagedArgs {
+    const void *q;
+    int64_t q_stride;
+    const void *k_new, *v_new;
+    int64_t kv_stride;
+    const int32_t *q_start, *seq_len, *table;
+    void *k, *v;
+    int n_pages, page_shift, max_pages;
+    int B, N, H, Hkv, group;
+    float scale_log2e;
+    int window, sinks;  // window 0: none
+    void *out;
+    float *part;        // [N][H][nsplit][DH + 2]: sums, maximum, normaliser (nsplit > 1)
+    int nsplit;
+    int64_t tiles;      // bound of the tiles of 16 rows
+};
+
+struct Sequence { int b, tile, start, m, len; };  // tile: number inside the sequence
+
+// The sequence that tile t lies in, sequences having tiles(m, len) tiles each: every wavefront adds them up, 64 sequences at a time.  What lies on the
+// device is clamped to what exists, so a bad table reads and writes nothing out of range.
+template <typename F> __device__ __forceinline__ bool find_sequence(const PagedArgs &a, int64_t t, F tiles, Sequence &s) {
+    const int lane = threadIdx.x % 64, most = a.max_pages << a.page_shift;
+    int64_t before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const int b = b0 + lane;
+        int start = 0, m = 0, len = 0, count = 0;
+        if (b < a.B) {
+            start = min(max(a.q_start[b], 0), a.N);
+            m = min(max(a.q_start[b + 1], start), a.N) - start;
+            len = min(max(a.seq_len[b], 0), most);
+            count = tiles(m, len);
+        }
+        const int upto = wave_scan(count), all = __builtin_amdgcn_readlane(upto, 63);
+        if (t < before + all) {
+            const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(before + upto > t));
+            s.b = b0 + src;
+            s.start = __builtin_amdgcn_readlane(start, src);
+            s.m = __builtin_amdgcn_readlane(m, src);
+            s.len = __builtin_amdgcn_readlane(len, src);
+            s.tile = (int)(t - before) - (__builtin_amdgcn_readlane(upto, src) - __builtin_amdgcn_readlane(count, src));
+            return true;
+        }
+        before += all;
+    }
+    return false;
+}
+
+__device__ __forceinline__ int page_of(const PagedArgs &a, int b, int key) { return a.table[(int64_t)b * a.max_pages + (key >> a.page_shift)]; }
+
+// New keys and values of 64 positions (counted from the sequence's first) and one key head.  Positions on a page number that does not exist are left out.
+template <typename T> __global__ __launch_bounds__(256) void paged_append(PagedArgs a, int dh) {
+    Sequence s;
+    const int64_t t = blockIdx.x / a.Hkv;
+    const int h = blockIdx.x % a.Hkv;
+    auto tiles = [&](int m, int len) {
+        const int first = max(len - m, 0);
+        return m > 0 && len > first ? (len - 1) / kAppendKeys - first / kAppendKeys + 1 : 0;
+    };
+    if (!find_sequence(a, t, tiles, s)) return;
+    const int base = s.len - s.m, first = max(base, 0);
+    const int k0 = max((first / kAppendKeys + s.tile) * kAppendKeys, first), k1 = min((first / kAppendKeys + s.tile + 1) * kAppendKeys, s.len);
+    const int page = 1 << a.page_shift;
+    for (int i = threadIdx.x; i < (k1 - k0) * dh; i += 256) {
+        const int key = k0 + i / dh, c = i % dh;
+        const int id = page_of(a, s.b, key), slot = key & (page - 1);
+        if (id < 0 || id >= a.n_pages) continue;
+        const int64_t head = (int64_t)id * a.Hkv + h;
+        const int64_t src = (int64_t)(s.start + key - base) * a.kv_stride + h * dh + c;
+        ((T *)a.k)[(head * page + slot) * dh + c] = ((const T *)a.k_new)[src];
+        ((T *)a.v)[(head * dh + c) * page + slot] = ((const T *)a.v_new)[src];
+    }
+}
+
+// The keys a tile of rows sees, in blocks of KB keys: blocks [0, first) hold the tokens that stay visible, blocks [from, from + count - first) the rest.
+struct Blocks {
+    int first, from, count;
+    __device__ __forceinline__ int at(int x) const { return x < first ? x : from + x - first; }
+};
+template <int KB> __device__ __forceinline__ Blocks visible_blocks(const PagedArgs &a, int p_lo, int p_hi) {
+    Blocks r = {0, 0, 0};
+    if (p_hi < 0) return r;
+    const int end = p_hi / KB + 1;
+    if (a.window) {
+        r.first = (min(a.sinks, p_hi + 1) + KB - 1) / KB;
+        r.from = max(max(p_lo - a.window + 1, 0) / KB, r.first);
+    }
+    r.count = r.first + max(end - r.from, 0);
+    return r;
+}
+__device__ __forceinline__ bool sees(const PagedArgs &a, int p, int key) { return key <= p && (!a.window || p - key < a.window || key < a.sinks); }
+
+// What a tile leaves of one row: the result, or this workgroup's share of it for the join.
+template <typename T, int DH> __device__ __forceinline__ T *out_row(const PagedArgs &a, int row, int head) { return (T *)a.out + ((int64_t)row * a.H + head) * DH; }
+template <int DH> __device__ __forceinline__ float *part_row(const PagedArgs &a, int row, int head, int split) {
+    return a.part + (((int64_t)row * a.H + head) * a.nsplit + split) * (DH + 2);
+}
+
+// One row over blocks [x0, x1), key by key: only visible keys and values are read.  The form for tiles whose sums are no numbers: where a key that
+// some rows do not see holds an infinity or a NaN, the tile's product with p = 0 would carry it into those rows.
+template <typename T, int DH, int KB>
+__device__ void plain_row(const PagedArgs &a, const Sequence &s, const Blocks &bl, int x0, int x1, int kvh, int row, int head, int p, int split) {
+    const int lane = threadIdx.x % 64, page = 1 << a.page_shift;
+    constexpr int E = (DH + 63) / 64;
+    const T *q = (const T *)a.q + (int64_t)row * a.q_stride + head * DH;
+    float qv[E], o[E], m = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; e++) {
+        qv[e] = lane + 64 * e < DH ? to_f(q[lane + 64 * e]) : 0.0f;
+        o[e] = 0.0f;
+    }
+    for (int x = x0; x < x1; x++)
+        for (int key = bl.at(x) * KB; key < bl.at(x) * KB + KB; key++) {
+            if (!sees(a, p, key) || key >= s.len) continue;
+            const int id = page_of(a, s.b, key), slot = key & (page - 1);
+            if (id < 0 || id >= a.n_pages) continue;
+            const int64_t hd = (int64_t)id * a.Hkv + kvh;
+            float dot = 0.0f, v[E];
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                const int c = lane + 64 * e;
+                v[e] = 0.0f;
+                if (c < DH) {
+                    dot = fmaf(qv[e], to_f(((const T *)a.k)[(hd * page + slot) * DH + c]), dot);
+                    v[e] = to_f(((const T *)a.v)[(hd * DH + c) * page + slot]);
+                }
+            }
+            dot = wave_sum(dot) * a.scale_log2e;
+            const float mn = dot > m ? dot : m;  // (a NaN stays out of the maximum and enters the sums through its term)
+            const float keep = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn), w = dot == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(dot - mn);
+            m = mn;
+            l = fmaf(l, keep, w);
+#pragma unroll
+            for (int e = 0; e < E; e++) o[e] = o[e] * keep + w * v[e];
+        }
+    float *part = a.nsplit > 1 ? part_row<DH>(a, row, head, split) : nullptr;
+#pragma unroll
+    for (int e = 0; e < E; e++) {
+        const int c = lane + 64 * e;
+        if (c >= DH) continue;
+        if (part) part[c] = o[e];
+        else out_row<T, DH>(a, row, head)[c] = from_f<T>(l == 0.0f ? 0.0f : o[e] / l);
+    }
+    if (part && lane == 0) {
+        part[DH] = m;
+        part[DH + 1] = l;
+    }
+}
+
+// Fragments of one block of keys as the two products take them.  bf16: v_mfma_f32_16x16x32_bf16, 32 keys; float32: v_mfma_f32_16x16x4_f32, 16 keys.
+// A lane holds row lane % 16 of the first operand and c = lane / 16 says which part of the contraction; of S^T it gets query lane % 16 and four rows.
+// bf16: key rows enter in an order that makes the eight keys a lane then holds of P consecutive, as its piece of V^T has them.
+template <typename T, int DH> struct Frags;
+template <int DH> struct Frags<bf16, DH> {
+    static constexpr int KB = 32, KF = (DH + 31) / 32, VF = DH / 16;
+    bf16x8 k[2][KF], v[VF];
+    __device__ __forceinline__ static bf16x8 zero() { return bf16x8{}; }
+    __device__ __forceinline__ static void load_q(bf16x8 (&q)[KF], const bf16 *row, bool valid) {
+        const int c = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int f = 0; f < KF; f++) {
+            q[f] = zero();
+            if (valid && 32 * f + 8 * c < DH) q[f] = *(const bf16x8 *)(row + 32 * f + 8 * c);
+        }
+    }
+    // key of the block behind row r of S^T's tile u
+    __device__ __forceinline__ static int key_of(int u, int r) { return 8 * (r / 4) + 4 * u + r % 4; }
+    __device__ __forceinline__ void load_k(const bf16 *const (&half)[2], int page) {  // half: this head's keys of 16 of the block's keys
+        const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            const int key = key_of(u, r);
+            const bf16 *src = (key < 16 ? half[0] : half[1]) + (key % 16) * DH + 8 * c;
+#pragma unroll
+            for (int f = 0; f < KF; f++) {
+                if (DH % 32 == 0 || 8 * c < DH) k[u][f] = *(const bf16x8 *)(src + 32 * f);
+                else k[u][f] = zero();
+            }
+        }
+    }
+    __device__ __forceinline__ void load_v(const bf16 *const (&half)[2], int page) {
+        const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
+        const bf16 *src = (c < 2 ? half[0] : half[1]) + (8 * c) % 16;
+#pragma unroll
+        for (int t = 0; t < VF; t++) v[t] = *(const bf16x8 *)(src + (16 * t + r) * page);
+    }
+    __device__ __forceinline__ void scores(floatx4 (&s)[2], const bf16x8 (&q)[KF]) const {
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            s[u] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int f = 0; f < KF; f++) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[u][f], q[f], s[u], 0, 0, 0);
+        }
+    }
+    __device__ __forceinline__ void add_values(floatx4 (&o)[VF], const floatx4 (&p)[2]) const {
+        bf16x8 w;  // (rounded once, as the operand of the matrix instruction; the normaliser adds the unrounded terms)
+#pragma unroll
+        for (int e = 0; e < 8; e++) w[e] = (bf16)p[e / 4][e % 4];
+#pragma unroll
+        for (int t = 0; t < VF; t++) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], w, o[t], 0, 0, 0);
+    }
+    // values of keys nobody in the tile may use (slots behind the last token): out of the product
+    __device__ __forceinline__ void drop_values(int from) {
+        const int c = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int t = 0; t < VF; t++)
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (8 * c + e >= from) v[t][e] = (bf16)0.0f;
+    }
+    static constexpr int TILES = 2;
+    using Q = bf16x8[KF];
+};
+template <int DH> struct Frags<float, DH> {
+    static constexpr int KB = 16, KF = DH / 16, VF = DH / 16;
+    floatx4 k[KF], v[VF];
+    __device__ __forceinline__ static void load_q(floatx4 (&q)[KF], const float *row, bool valid) {
+        const int c = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int f = 0; f < KF; f++) {
+            q[f] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (valid) q[f] = *(const floatx4 *)(row + 16 * f + 4 * c);
+        }
+    }
+    __device__ __forceinline__ static int key_of(int, int r) { return r; }
+    __device__ __forceinline__ void load_k(const float *const (&half)[2], int page) {
+        const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int f = 0; f < KF; f++) k[f] = *(const floatx4 *)(half[0] + r * DH + 16 * f + 4 * c);
+    }
+    __device__ __forceinline__ void load_v(const float *const (&half)[2], int page) {
+        const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int t = 0; t < VF; t++) v[t] = *(const floatx4 *)(half[0] + (16 * t + r) * page + 4 * c);
+    }
+    __device__ __forceinline__ void scores(floatx4 (&s)[1], const floatx4 (&q)[KF]) const {
+        s[0] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int f = 0; f < KF; f++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[f][e], q[f][e], s[0], 0, 0, 0);
+    }
+    __device__ __forceinline__ void add_values(floatx4 (&o)[VF], const floatx4 (&p)[1]) const {
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+#pragma unroll
+            for (int t = 0; t < VF; t++) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][e], p[0][e], o[t], 0, 0, 0);
+    }
+    __device__ __forceinline__ void drop_values(int from) {
+        const int c = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int t = 0; t < VF; t++)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (4 * c + e >= from) v[t][e] = 0.0f;
+    }
+    static constexpr int TILES = 1;
+    using Q = floatx4[KF];
+};
+
+// maximum and sum over the four lanes that hold one query's scores
+__device__ __forceinline__ float query_max(float v) {
+    v = halves_max(v);
+    const uintx2 p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float query_sum(float v) {
+    v = halves_sum(v);
+    const uintx2 p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
+template <typename T, int DH> __global__ __launch_bounds__(256) void paged_rows(PagedArgs a) {
+    using F = Frags<T, DH>;
+    constexpr int KB = F::KB, VF = F::VF, NW = 4;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, c = lane / 16;
+    const int split = blockIdx.x % a.nsplit, kvh = blockIdx.x / a.nsplit % a.Hkv, page = 1 << a.page_shift;
+    Sequence s;
+    if (!find_sequence(a, blockIdx.x / (a.nsplit * a.Hkv), [&](int m, int) { return (m * a.group + kRows - 1) / kRows; }, s)) return;
+    const int R0 = s.tile * kRows, R1 = min(R0 + kRows, s.m * a.group), base = s.len - s.m;
+    const int p_lo = base + R0 / a.group, p_hi = base + (R1 - 1) / a.group;
+    const Blocks bl = visible_blocks<KB>(a, p_lo, p_hi);
+    const int each = (bl.count + a.nsplit * NW - 1) / (a.nsplit * NW);
+    const int x0 = min((split * NW + wave) * each, bl.count), x1 = min(x0 + each, bl.count);
+
+    const int R = R0 + n, tok = R / a.group, head = kvh * a.group + R - tok * a.group, p = R < R1 ? base + tok : -1;
+    typename F::Q q;
+    F::load_q(q, (const T *)a.q + (int64_t)(s.start + tok) * a.q_stride + head * DH, R < R1);
+
+    // page numbers: one of 64 successive pages per lane
+    int ids = 0, ids_from = -64;
+    auto page_id = [&](int pg) {
+        if (pg < ids_from || pg >= ids_from + 64) {
+            ids_from = pg;
+            const int at = pg + lane;
+            ids = at < a.max_pages ? a.table[(int64_t)s.b * a.max_pages + at] : -1;
+        }
+        return __builtin_amdgcn_readlane(ids, pg - ids_from);
+    };
+    struct Source { const T *k[2], *v[2]; int valid; };  // valid: bit i: keys 16 i .. 16 i + 15 of the block lie on a page that exists
+    auto source = [&](int x) {
+        Source r;
+        r.valid = 0;
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+            const int key = bl.at(x) * KB + (KB == 32 ? 16 * i : 0), slot = key & (page - 1);
+            int id = (key >> a.page_shift) < a.max_pages ? page_id(key >> a.page_shift) : -1;
+            if (id >= 0 && id < a.n_pages) r.valid |= 1 << i;
+            else id = 0;
+            const int64_t hd = (int64_t)id * a.Hkv + kvh;
+            r.k[i] = (const T *)a.k + (hd * page + slot) * DH;
+            r.v[i] = (const T *)a.v + hd * DH * page + slot;
+        }
+        return r;
+    };
+
+    F f;
+    floatx4 o[VF];
+#pragma unroll
+    for (int t = 0; t < VF; t++) o[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    float m_run = -INFINITY, l_run = 0.0f;
+    Source src = {};
+    if (x0 < x1) {
+        src = source(x0);
+        f.load_k(src.k, page);
+        f.load_v(src.v, page);
+    }
+    for (int x = x0; x < x1; x++) {
+        const int key0 = bl.at(x) * KB, valid = src.valid;
+        floatx4 sc[F::TILES];
+        f.scores(sc, q);
+        if (x + 1 < x1) {
+            src = source(x + 1);
+            f.load_k(src.k, page);
+        }
+        const bool whole = valid == 3 && key0 + KB - 1 <= p_lo && (!a.window || p_hi - key0 < a.window || key0 + KB <= a.sinks);
+        if (!whole) {
+#pragma unroll
+            for (int u = 0; u < F::TILES; u++)
+#pragma unroll
+                for (int v = 0; v < 4; v++) {
+                    const int kk = F::key_of(u, 4 * c + v);
+                    if (!sees(a, p, key0 + kk) || !(valid >> (kk / 16) & 1)) sc[u][v] = -INFINITY;
+                }
+            if (key0 + KB - 1 > p_hi) f.drop_values(p_hi + 1 - key0);
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < F::TILES; u++)
+#pragma unroll
+            for (int v = 0; v < 4; v++) mx = fmaxf(mx, sc[u][v]);
+        mx = query_max(mx) * a.scale_log2e;
+        // the maximum in use follows when it is outgrown by 2^8: terms up to 256 harm nothing
+        if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0) {
+            const float mn = mx > m_run + 8.0f ? mx : m_run;
+            const float alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - mn);
+            m_run = mn;
+            l_run *= alpha;
+#pragma unroll
+            for (int t = 0; t < VF; t++)
+#pragma unroll
+                for (int v = 0; v < 4; v++) o[t][v] *= alpha;
+        }
+        const float neg = m_run == -INFINITY ? 0.0f : -m_run;
+#pragma unroll
+        for (int u = 0; u < F::TILES; u++)
+#pragma unroll
+            for (int v = 0; v < 4; v++) {
+                sc[u][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u][v], a.scale_log2e, neg));
+                l_run += sc[u][v];
+            }
+        f.add_values(o, sc);
+        if (x + 1 < x1) f.load_v(src.v, page);
+    }
+    l_run = query_sum(l_run);
+
+    // the wavefronts' stretches, joined in their order
+    __shared__ float sm[NW][kRows], sl[NW][kRows];
+    __shared__ __attribute__((aligned(16))) float so[NW][kRows][DH + 4];
+    if (c == 0) {
+        sm[wave][n] = m_run;
+        sl[wave][n] = l_run;
+    }
+#pragma unroll
+    for (int t = 0; t < VF; t++) *(floatx4 *)&so[wave][n][16 * t + 4 * c] = o[t];
+    __syncthreads();
+    bool bad = false;
+    for (int i = threadIdx.x; i < kRows * DH; i += 256) {
+        const int r = i / DH, d = i % DH, RR = R0 + r;
+        if (RR >= R1) continue;
+        float m = sm[0][r];
+#pragma unroll
+        for (int w = 1; w < NW; w++) m = fmaxf(m, sm[w][r]);
+        float l = 0.0f, v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; w++) {
+            const float f_ = sm[w][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][r] - m);
+            l = fmaf(sl[w][r], f_, l);
+            v = fmaf(so[w][r][d], f_, v);
+            bad |= !(fabsf(so[w][r][d]) < INFINITY) || !(sl[w][r] < INFINITY);
+        }
+        const int tk = RR / a.group, row = s.start + tk, hd = kvh * a.group + RR - tk * a.group;
+        if (a.nsplit > 1) {
+            float *part = part_row<DH>(a, row, hd, split);
+            part[d] = v;
+            if (d == 0) {
+                part[DH] = m;
+                part[DH + 1] = l;
+            }
+        } else {
+            out_row<T, DH>(a, row, hd)[d] = from_f<T>(l == 0.0f ? 0.0f : v / l);
+        }
+    }
+    if (__syncthreads_or(bad)) {
+        const int y0 = min(split * NW * each, bl.count), y1 = min(y0 + NW * each, bl.count);
+        for (int r = wave; r < R1 - R0; r += NW) {
+            const int RR = R0 + r, tk = RR / a.group;
+            plain_row<T, DH, KB>(a, s, bl, y0, y1, kvh, s.start + tk, kvh * a.group + RR - tk * a.group, base + tk, split);
+        }
+    }
+}
+
+// Joins the workgroups' shares of a row: one wavefront per row.
+template <typename T, int DH> __global__ __launch_bounds__(256) void paged_join(PagedArgs a) {
+    const int lane = threadIdx.x % 64;
+    const int64_t w = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;  // (tile, key head, row)
+    const int r = (int)(w % kRows), kvh = (int)(w / kRows % a.Hkv);
+    Sequence s;
+    if (!find_sequence(a, w / (kRows * a.Hkv), [&](int m, int) { return (m * a.group + kRows - 1) / kRows; }, s)) return;
+    const int R = s.tile * kRows + r;
+    if (R >= s.m * a.group) return;
+    const int tok = R / a.group, row = s.start + tok, head = kvh * a.group + R - tok * a.group;
+    constexpr int E = (DH + 63) / 64;
+    const float *part = part_row<DH>(a, row, head, 0);
+    float m = -INFINITY;
+    for (int i = lane; i < a.nsplit; i += 64) m = fmaxf(m, part[(int64_t)i * (DH + 2) + DH]);
+    m = wave_max(m);
+    float l = 0.0f, o[E] = {};
+    for (int i = 0; i < a.nsplit; i++) {
+        const float *x = part + (int64_t)i * (DH + 2);
+        const float mi = x[DH], f = mi == m ? 1.0f : __builtin_amdgcn_exp2f(mi - m);
+        l = fmaf(x[DH + 1], f, l);
+#pragma unroll
+        for (int e = 0; e < E; e++)
+            if (lane + 64 * e < DH) o[e] = fmaf(x[lane + 64 * e], f, o[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < E; e++)
+        if (lane + 64 * e < DH) out_row<T, DH>(a, row, head)[lane + 64 * e] = from_f<T>(l == 0.0f ? 0.0f : o[e] / l);
+}
+
+int shift_of(int page) {
+    int s = 0;
+    while ((1 << s) < page) s++;
+    return s;
+}
+
+// Stretches of the keys that workgroups of their own walk.
+int splits_of(int64_t tiles, int Hkv, int64_t most_keys) {
+    const int64_t want = (2048 + tiles * Hkv - 1) / (tiles * Hkv), most = (most_keys + 255) / 256;
+    const int64_t n = want < most ? want : most;
+    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+}
+
+struct Plan { int64_t tiles; int nsplit; size_t bytes; };
+Plan plan_of(int B, int N, int H, int Hkv, int dh, int page, int max_pages, int window, int sinks) {
+    Plan p;
+    p.tiles = (int64_t)N * (H / Hkv) / kRows + B;
+    if (p.tiles > (int64_t)N * (H / Hkv)) p.tiles = (int64_t)N * (H / Hkv);
+    int64_t keys = (int64_t)max_pages * page;
+    if (window && (int64_t)window + sinks + 64 < keys) keys = (int64_t)window + sinks + 64;
+    p.nsplit = splits_of(p.tiles, Hkv, keys);
+    p.bytes = p.nsplit > 1 ? (size_t)N * H * p.nsplit * (dh + 2) * sizeof(float) : 0;
+    return p;
+}
+
+template <typename T, int DH> int launch_rows(const PagedArgs &a, hipStream_t st) {
+    const int64_t grid = a.tiles * a.Hkv * a.nsplit;
+    if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
+    hipLaunchKernelGGL((paged_rows<T, DH>), dim3((unsigned)grid), dim3(256), 0, st, a);
+    GR4AD_LAUNCH_CHECK();
+    if (a.nsplit > 1) {
+        hipLaunchKernelGGL((paged_join<T, DH>), dim3((unsigned)(a.tiles * a.Hkv * kRows / 4)), dim3(256), 0, st, a);
+        GR4AD_LAUNCH_CHECK();
+    }
+    return GR4AD_OK;
+}
+template <typename T> int launch_width(const PagedArgs &a, int dh, hipStream_t st) {
+    switch (dh) {
+        case 16: return launch_rows<T, 16>(a, st);
+        case 32: return launch_rows<T, 32>(a, st);
+        case 64: return launch_rows<T, 64>(a, st);
+        default: return launch_rows<T, 128>(a, st);
+    }
+}
+
+const int kMostKeys = 1 << 30;  // positions and their differences stay in 32 bits
+
+// what both entry points check; a message and a status for the caller
+int check_shape(gr4ad_dtype dtype, const gr4ad_paged_cache *c, int32_t B, int32_t N, int32_t H, int32_t window, int32_t sinks) {
+    if (!c) return gr4ad_set_thread_error(GR4AD_EINVAL, "paged attention: cache is NULL");
+    if (dtype != GR4AD_F32 && dtype != GR4AD_BF16) return gr4ad_set_thread_error(GR4AD_EINVAL, "paged attention: dtype %d", (int)dtype);
+    if (B < 1 || N < 1 || H < 1 || c->H_kv < 1 || c->n_pages < 1 || c->max_pages < 1 || window < 0 || sinks < 0)
+        return gr4ad_set_thread_error(GR4AD_EINVAL, "paged attention: sizes must be positive (B %d, N %d, H %d, H_kv %d, n_pages %d, max_pages %d), window %d and sinks %d not negative", B, N, H,
+                                      c->H_kv, c->n_pages, c->max_pages, window, sinks);
+    if (H % c->H_kv) return gr4ad_set_thread_error(GR4AD_EINVAL, "paged attention: H = %d is not divisible by H_kv = %d", H, c->H_kv);
+    if (c->dh != 16 && c->dh != 32 && c->dh != 64 && c->dh != 128) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: head width %d (16, 32, 64, 128)", c->dh);
+    if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
+        return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: page_size %d is not a power of two from 16 to 1024", c->page_size);
+    if ((int64_t)c->max_pages * c->page_size > kMostKeys || (int64_t)N * H > kMostKeys || (int64_t)B * c->H_kv > kMostKeys)
+        return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: more than 2^30 positions of a sequence, rows times heads or sequences times heads");
+    return GR4AD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t gr4ad_op_paged_attention_workspace_bytes(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, int32_t B, int32_t N, int32_t H, int32_t window, int32_t sinks) {
+    if (check_shape(dtype, cache, B, N, H, window, sinks)) return 0;
+    return plan_of(B, N, H, cache->H_kv, cache->dh, cache->page_size, cache->max_pages, window, sinks).bytes;
+}
+
+int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, const void *q, int64_t q_stride, const void *k_new, const void *v_new, int64_t kv_stride,
+                             const int32_t *q_start, const int32_t *seq_len, void *out, int32_t B, int32_t N, int32_t H, float scale, int32_t window, int32_t sinks,
+                             void *workspace, size_t workspace_bytes, void *hip_stream) {
+    int s = check_shape(dtype, cache, B, N, H, window, sinks);
+    if (s) return s;
+    const gr4ad_paged_cache &c = *cache;
+    if (!q || !q_start || !seq_len || !out || !c.k_pages || !c.v_pages || !c.page_table || !k_new != !v_new)
+        return gr4ad_set_thread_error(GR4AD_EINVAL, "paged attention: NULL pointer (k_new and v_new: both or neither)");
+    if (!(scale > 0.0f) || !(scale < INFINITY)) return gr4ad_set_thread_error(GR4AD_EINVAL, "paged attention: scale must be positive and finite");
+    const int piece = dtype == GR4AD_BF16 ? 8 : 4;
+    if (q_stride < (int64_t)H * c.dh || (k_new && kv_stride < (int64_t)c.H_kv * c.dh)) return gr4ad_set_thread_error(GR4AD_EINVAL, "paged attention: rows overlap (strides in elements)");
+    if (q_stride % piece || kv_stride % piece || (uintptr_t)k_new % 16 || (uintptr_t)v_new % 16 || (uintptr_t)q % 16 || (uintptr_t)c.k_pages % 16 || (uintptr_t)c.v_pages % 16 || (uintptr_t)out % 16)
+        return gr4ad_set_thread_error(GR4AD_EINVAL, "paged attention: q, k_new, v_new, their rows, the pages and out must be 16-byte aligned");
+    const Plan p = plan_of(B, N, H, c.H_kv, c.dh, c.page_size, c.max_pages, window, sinks);
+    if (p.bytes && (!workspace || workspace_bytes < p.bytes || (uintptr_t)workspace % 16))
+        return gr4ad_set_thread_error(GR4AD_EWORKSPACE, "paged attention: workspace of %zu bytes needed, 16-byte aligned", p.bytes);
+    hipStream_t st = (hipStream_t)hip_stream;
+    PagedArgs a = {q, q_stride, k_new, v_new, kv_stride, q_start, seq_len, c.page_table, c.k_pages, c.v_pages, c.n_pages, shift_of(c.page_size), c.max_pages, B, N, H, c.H_kv,
+                   H / c.H_kv, scale * 1.4426950408889634f, window > kMostKeys ? kMostKeys : window, sinks > kMostKeys ? kMostKeys : sinks, out, (float *)workspace, p.nsplit, p.tiles};
+    const int e = dtype == GR4AD_BF16 ? 2 : 4;
+    if (k_new) {
+        int64_t tiles = (int64_t)N / kAppendKeys + 2 * (int64_t)B;
+        if (tiles > N) tiles = N;
+        const int64_t grid = tiles * c.H_kv;
+        if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
+        ProfScope ps(KC_PAGED_APPEND, st, 0.0, 4.0 * N * c.H_kv * c.dh * e);
+        if (dtype == GR4AD_BF16) hipLaunchKernelGGL(paged_append<bf16>, dim3((unsigned)grid), dim3(256), 0, st, a, c.dh);
+        else hipLaunchKernelGGL(paged_append<float>, dim3((unsigned)grid), dim3(256), 0, st, a, c.dh);
+        GR4AD_LAUNCH_CHECK();
+    }
+    // lengths lie on the device: counted on all pages of every sequence, an upper bound
+    const double keys = (double)c.max_pages * c.page_size;
+    ProfScope ps(KC_PAGED_ATTN, st, 4.0 * N * keys * H * c.dh, e * (2.0 * B * keys * c.H_kv * c.dh + 2.0 * N * H * c.dh));
+    return dtype == GR4AD_BF16 ? launch_width<bf16>(a, c.dh, st) : launch_width<float>(a, c.dh, st);
+}
+
+}  // extern "C"

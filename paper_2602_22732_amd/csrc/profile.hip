@@ -21,7 +21,8 @@ thread_local int64_t t_rows = 0;
 const char *kNames[KC_COUNT] = {"gemm_bf16_tile", "gemm_simple", "cross_attn_flash_bf16",
                                 "cross_attn_simple", "self_attn_step", "trunk_self_attn", "rmsnorm", "fuse_gate", "select_rows",
                                 "select_request", "gather_rows", "broadcast_rows", "v_transpose", "gemm_bf16_ring", "masked_softmax_rows",
-                                "gemm_fp8_ring", "quantize_rows", "context_attn_flash_bf16", "distinct_rows"};
+                                "gemm_fp8_ring", "quantize_rows", "context_attn_flash_bf16", "distinct_rows",
+                                "paged_append", "paged_attention", "quantize_blocks", "gemm_fp8_block", "adjust_logits"};
 }  // namespace
 
 ProfScope::ProfScope(int cls, hipStream_t st, double flops, double bytes) : idx_(-1), st_(st) {
