@@ -412,123 +412,122 @@ def op_gather_rows(src, parent, k=None, row_elems=None, stream=None):
 
 
 # ---- an autoregressive step's operators: attention over pages, block-scaled FP8 products, logits in front of the selection
-# These check devices, types, shapes and strides before the library sees a pointer, launch on `stream` (default: the current one of the operands' device),
-# and hold what they allocate themselves for that stream.
-def _operands(what, first, *rest):
-    """ValueError unless every tensor (None is passed over) lies on the GPU of `first`."""
-    dev = first.device
-    if dev.type != "cuda":
-        raise ValueError("%s: tensors on the GPU are needed, got %s" % (what, dev))
+# These check devices, types, shapes and strides before the library sees a pointer and launch on `stream` (default: the current one of the operands' device),
+# for which they also allocate what is theirs.  A short call is bound by this side, so the checks are written to cost little where they hold.
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _place(what, first, stream, rest):
+    """None if the call can go on: every tensor (None is passed over) lies on the current GPU and the current stream is meant.  Otherwise the context to
+    make the call in; ValueError for tensors on several devices or none."""
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError("%s: tensors on the GPU are needed, got %s" % (what, first.device))
     for t in rest:
-        if t is not None and t.device != dev:
-            raise ValueError("%s: tensors on %s and %s" % (what, dev, t.device))
+        if t is not None and t.get_device() != dev:
+            raise ValueError("%s: tensors on %s and %s" % (what, first.device, t.device))
+    if stream is None:
+        return None if dev == _device() else torch.cuda.device(dev)
+    if stream.device.index != dev:
+        raise ValueError("%s: tensors on %s, a stream of %s" % (what, first.device, stream.device))
+    return torch.cuda.stream(stream)  # (makes its device the current one, too)
 
 
-def _typed(what, t, dtype, shape):
-    """ValueError unless t (None is passed over) is dense, of the type and of the shape (None: any size)."""
-    if t is None:
-        return
-    if t.dtype != dtype or t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)) or not t.is_contiguous():
-        raise ValueError("%s: needs a dense %s tensor of shape %s, got %s %s%s" % (what, dtype, tuple(shape), t.dtype, tuple(t.shape),
-                                                                                   "" if t.is_contiguous() else " (strided)"))
+def _dense(what, name, t, dtype, shape):
+    """ValueError unless t is None or dense, of the type and of the shape."""
+    if t is not None and not (t.dtype is dtype and t.shape == shape and t.is_contiguous()):
+        raise ValueError("%s: %s must be dense %s %s, got %s %s%s" % (what, name, dtype, tuple(shape), t.dtype, tuple(t.shape), "" if t.is_contiguous() else " (strided)"))
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-class _On:
-    """The device and stream of a call: what is allocated and launched inside belongs to them."""
-
-    def __init__(self, device, stream):
-        self.device = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
-        self.given = stream
-
-    def __enter__(self):
-        if self.device:
-            self.device.__enter__()
-        self.stream = torch.cuda.stream(self.given) if self.given is not None else None
-        if self.stream:
-            self.stream.__enter__()
-        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
-
-    def __exit__(self, *e):
-        if self.stream:
-            self.stream.__exit__(*e)
-        if self.device:
-            self.device.__exit__(*e)
-
-
 def op_paged_attention(q, k_pages, v_pages, page_table, q_start, seq_len, k_new=None, v_new=None, scale=None, window=0, sinks=0, out=None, workspace=None, stream=None):
     """gr4ad_op_paged_attention: q [N,H,dh] (rows may be strided), k_pages [n_pages,H_kv,page_size,dh], v_pages [n_pages,H_kv,dh,page_size], page_table
     [B,max_pages], q_start [B+1], seq_len [B] int32; k_new, v_new [N,H_kv,dh] are written into their pages first.  scale: 1/sqrt(dh) if None."""
     what = "op_paged_attention"
-    _operands(what, q, k_pages, v_pages, page_table, q_start, seq_len, k_new, v_new, out, workspace)
-    if q.dtype not in (torch.float32, torch.bfloat16) or q.dim() != 3 or k_pages.dim() != 4 or page_table.dim() != 2:
+    at = _place(what, q, stream, (k_pages, v_pages, page_table, q_start, seq_len, k_new, v_new, out, workspace))
+    if at is not None:
+        with at:
+            return op_paged_attention(q, k_pages, v_pages, page_table, q_start, seq_len, k_new, v_new, scale, window, sinks, out, workspace)
+    dtype = q.dtype
+    if dtype not in (torch.float32, torch.bfloat16) or q.dim() != 3 or k_pages.dim() != 4 or page_table.dim() != 2:
         raise ValueError("%s: q [N,H,dh] float32 or bfloat16, k_pages [n_pages,H_kv,page_size,dh], page_table [B,max_pages]" % what)
     N, H, dh = q.shape
     n_pages, H_kv, page, _ = k_pages.shape
     B, max_pages = page_table.shape
-    _typed(what + " k_pages", k_pages, q.dtype, (None, None, None, dh))
-    _typed(what + " v_pages", v_pages, q.dtype, (n_pages, H_kv, dh, page))
-    _typed(what + " page_table", page_table, torch.int32, (None, None))
-    _typed(what + " q_start", q_start, torch.int32, (B + 1,))
-    _typed(what + " seq_len", seq_len, torch.int32, (B,))
-    _typed(what + " out", out, q.dtype, (N, H, dh))
+    i32 = torch.int32
+    _dense(what, "k_pages", k_pages, dtype, (n_pages, H_kv, page, dh))
+    _dense(what, "v_pages", v_pages, dtype, (n_pages, H_kv, dh, page))
+    _dense(what, "page_table", page_table, i32, (B, max_pages))
+    _dense(what, "q_start", q_start, i32, (B + 1,))
+    _dense(what, "seq_len", seq_len, i32, (B,))
+    _dense(what, "out", out, dtype, (N, H, dh))
+    strides = []
     for name, t, heads in (("q", q, H), ("k_new", k_new, H_kv), ("v_new", v_new, H_kv)):
-        if t is not None and (t.dtype != q.dtype or tuple(t.shape) != (N, heads, dh) or t.stride(2) != 1 or (heads > 1 and t.stride(1) != dh)):
-            raise ValueError("%s: %s must be %s [%d,%d,%d] with dense rows, got %s %s strides %s" % (what, name, q.dtype, N, heads, dh, t.dtype, tuple(t.shape), t.stride()))
-    row = lambda t, heads: t.stride(0) if N > 1 else heads * dh  # noqa: E731
-    kv_stride = 0 if k_new is None else row(k_new, H_kv)
-    if k_new is not None and v_new is not None and row(v_new, H_kv) != kv_stride:
-        raise ValueError("%s: rows of k_new and v_new lie %d and %d values apart" % (what, kv_stride, row(v_new, H_kv)))
+        if t is None:
+            strides.append(None)
+            continue
+        row, head, one = t.stride()
+        if t.dtype is not dtype or t.shape != (N, heads, dh) or one != 1 or (heads > 1 and head != dh):
+            raise ValueError("%s: %s must be %s [%d,%d,%d] with dense rows, got %s %s strides %s" % (what, name, dtype, N, heads, dh, t.dtype, tuple(t.shape), t.stride()))
+        strides.append(row if N > 1 else heads * dh)
+    if k_new is not None and v_new is not None and strides[1] != strides[2]:
+        raise ValueError("%s: rows of k_new and v_new lie %d and %d values apart" % (what, strides[1], strides[2]))
     L = lib()
-    cache = PagedCacheDesc(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), n_pages, page, max_pages, H_kv, dh)
-    dt = dtype_code(q.dtype)
-    with _On(q.device, stream) as st:
-        if out is None:
-            out = torch.empty(N, H, dh, dtype=q.dtype, device=q.device)
-        if workspace is None:
-            need = int(L.gr4ad_op_paged_attention_workspace_bytes(dt, C.byref(cache), B, N, H, window, sinks))
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-        _check(L.gr4ad_op_paged_attention(dt, C.byref(cache), q.data_ptr(), row(q, H), _ptr(k_new), _ptr(v_new), kv_stride, q_start.data_ptr(), seq_len.data_ptr(),
-                                          out.data_ptr(), B, N, H, dh ** -0.5 if scale is None else scale, window, sinks, _ptr(workspace),
-                                          workspace.numel() * workspace.element_size() if workspace is not None else 0, st))
+    cache = C.byref(PagedCacheDesc(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), n_pages, page, max_pages, H_kv, dh))
+    dt = BF16 if dtype is torch.bfloat16 else F32
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if workspace is None:
+        need = L.gr4ad_op_paged_attention_workspace_bytes(dt, cache, B, N, H, window, sinks)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _check(L.gr4ad_op_paged_attention(dt, cache, q.data_ptr(), strides[0], _ptr(k_new), _ptr(v_new), strides[1] or 0, q_start.data_ptr(), seq_len.data_ptr(), out.data_ptr(), B, N, H,
+                                      dh ** -0.5 if scale is None else scale, window, sinks, _ptr(workspace),
+                                      0 if workspace is None else workspace.numel() * workspace.element_size(), _raw_stream(_device())))
     return out
 
 
 def op_quantize_blocks(x, block_rows=1, stream=None):
     """x [rows, n] float32 or bf16 (rows may be strided) -> (q [rows, n] uint8 holding E4M3 bytes, scale [ceil(n/128), ceil(rows/block_rows)] float32)."""
-    _operands("op_quantize_blocks", x)
-    if x.dtype not in (torch.float32, torch.bfloat16) or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1) or block_rows not in (1, 128):
-        raise ValueError("op_quantize_blocks: x [rows, n] float32 or bfloat16 with dense rows, block_rows 1 or 128; got %s %s strides %s, %r" % (x.dtype, tuple(x.shape), x.stride(), block_rows))
+    at = _place("op_quantize_blocks", x, stream, ())
+    if at is not None:
+        with at:
+            return op_quantize_blocks(x, block_rows)
+    dtype = x.dtype
+    if dtype not in (torch.float32, torch.bfloat16) or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1) or block_rows not in (1, 128):
+        raise ValueError("op_quantize_blocks: x [rows, n] float32 or bfloat16 with dense rows, block_rows 1 or 128; got %s %s strides %s, %r" % (dtype, tuple(x.shape), x.stride(), block_rows))
     rows, n = x.shape
-    with _On(x.device, stream) as st:
-        q = torch.empty(rows, n, dtype=torch.uint8, device=x.device)
-        scale = torch.empty(-(-n // 128), -(-rows // block_rows), dtype=torch.float32, device=x.device)
-        _check(lib().gr4ad_op_quantize_blocks(dtype_code(x.dtype), x.data_ptr(), x.stride(0) if rows > 1 else n, q.data_ptr(), scale.data_ptr(), rows, n, block_rows, st))
+    q = torch.empty(rows, n, dtype=torch.uint8, device=x.device)
+    scale = torch.empty(-(-n // 128), -(-rows // block_rows), dtype=torch.float32, device=x.device)
+    _check(lib().gr4ad_op_quantize_blocks(BF16 if dtype is torch.bfloat16 else F32, x.data_ptr(), x.stride(0) if rows > 1 else n, q.data_ptr(), scale.data_ptr(), rows, n, block_rows,
+                                          _raw_stream(_device())))
     return q, scale
 
 
 def op_linear_fp8_block(Aq, a_scale, Wq, w_scale, bias=None, out_dtype=torch.bfloat16, out=None, stream=None):
     """gr4ad_op_linear_fp8_block on the outputs of op_quantize_blocks (block_rows 1 for Aq [M,K], 128 for Wq [N,K]); out_dtype bfloat16 or float16."""
     what = "op_linear_fp8_block"
-    _operands(what, Aq, a_scale, Wq, w_scale, bias, out)
-    if out_dtype not in (torch.bfloat16, torch.float16):
-        raise ValueError("%s: out_dtype bfloat16 or float16, got %s" % (what, out_dtype))
-    _typed(what + " Aq", Aq, torch.uint8, (None, None))
+    at = _place(what, Aq, stream, (a_scale, Wq, w_scale, bias, out))
+    if at is not None:
+        with at:
+            return op_linear_fp8_block(Aq, a_scale, Wq, w_scale, bias, out_dtype, out)
+    if out_dtype not in (torch.bfloat16, torch.float16) or Aq.dim() != 2 or Wq.dim() != 2:
+        raise ValueError("%s: Aq [M,K], Wq [N,K], out_dtype bfloat16 or float16" % what)
     M, K = Aq.shape
-    _typed(what + " Wq", Wq, torch.uint8, (None, K))
-    N = Wq.shape[0]
-    _typed(what + " a_scale", a_scale, torch.float32, (-(-K // 128), M))
-    _typed(what + " w_scale", w_scale, torch.float32, (-(-K // 128), -(-N // 128)))
-    _typed(what + " bias", bias, torch.float32, (N,))
-    _typed(what + " out", out, out_dtype, (M, N))
-    with _On(Aq.device, stream) as st:
-        if out is None:
-            out = torch.empty(M, N, dtype=out_dtype, device=Aq.device)
-        _check(lib().gr4ad_op_linear_fp8_block(Aq.data_ptr(), a_scale.data_ptr(), Wq.data_ptr(), w_scale.data_ptr(), _ptr(bias), out.data_ptr(), M, N, K,
-                                               int(out_dtype == torch.float16), st))
+    N, nb = Wq.shape[0], -(-K // 128)
+    _dense(what, "Aq", Aq, torch.uint8, (M, K))
+    _dense(what, "Wq", Wq, torch.uint8, (N, K))
+    _dense(what, "a_scale", a_scale, torch.float32, (nb, M))
+    _dense(what, "w_scale", w_scale, torch.float32, (nb, -(-N // 128)))
+    _dense(what, "bias", bias, torch.float32, (N,))
+    _dense(what, "out", out, out_dtype, (M, N))
+    if out is None:
+        out = torch.empty(M, N, dtype=out_dtype, device=Aq.device)
+    _check(lib().gr4ad_op_linear_fp8_block(Aq.data_ptr(), a_scale.data_ptr(), Wq.data_ptr(), w_scale.data_ptr(), _ptr(bias), out.data_ptr(), M, N, K,
+                                           1 if out_dtype is torch.float16 else 0, _raw_stream(_device())))
     return out
 
 
@@ -538,27 +537,50 @@ def op_adjust_logits(logits, history=None, history_len=None, repetition=None, pr
     history [rows, most] int32, history_len / bias_row / mask_row [rows] int32, repetition / presence / frequency [rows] float32, bias [n, V] float32,
     mask [n, ceil(V/32)] int32 (bit v % 32 of word v // 32 set: token v is allowed)."""
     what = "op_adjust_logits"
-    _operands(what, logits, history, history_len, repetition, presence, frequency, bias, bias_row, mask, mask_row, out)
-    if logits.dtype not in (torch.float32, torch.float16) or logits.dim() < 1 or not logits.is_contiguous():
-        raise ValueError("%s: dense float32 or float16 logits [..., V], got %s %s" % (what, logits.dtype, tuple(logits.shape)))
-    V = logits.shape[-1]
+    at = _place(what, logits, stream, (history, history_len, repetition, presence, frequency, bias, bias_row, mask, mask_row, out))
+    if at is not None:
+        with at:
+            return op_adjust_logits(logits, history, history_len, repetition, presence, frequency, bias, bias_row, mask, mask_row, out)
+    dtype, shape, i32, f32 = logits.dtype, logits.shape, torch.int32, torch.float32
+    if dtype not in (f32, torch.float16) or len(shape) < 1 or not logits.is_contiguous():
+        raise ValueError("%s: dense float32 or float16 logits [..., V], got %s %s" % (what, dtype, tuple(shape)))
+    V = shape[-1]
     rows = logits.numel() // V if V else 0
-    _typed(what + " out", out, logits.dtype, logits.shape)
-    _typed(what + " history", history, torch.int32, (rows, None))
-    _typed(what + " bias", bias, torch.float32, (None, V))
-    _typed(what + " mask", mask, torch.int32, (None, -(-V // 32)))
-    for name, t, dt in (("history_len", history_len, torch.int32), ("bias_row", bias_row, torch.int32), ("mask_row", mask_row, torch.int32),
-                        ("repetition", repetition, torch.float32), ("presence", presence, torch.float32), ("frequency", frequency, torch.float32)):
-        if t is not None:
-            _typed("%s %s" % (what, name), t, dt, (rows,))
+    one = (rows,)
+    rules = LogitRules()
+    if history is not None:
+        _dense(what, "history", history, i32, (rows, history.shape[-1]))
+        rules.history, rules.history_stride = history.data_ptr(), history.shape[1]
+    if bias is not None:
+        _dense(what, "bias", bias, f32, (bias.shape[0], V))
+        rules.bias, rules.n_bias = bias.data_ptr(), bias.shape[0]
+    if mask is not None:
+        _dense(what, "mask", mask, i32, (mask.shape[0], -(-V // 32)))
+        rules.mask, rules.n_masks = mask.data_ptr(), mask.shape[0]
+    if history_len is not None:
+        _dense(what, "history_len", history_len, i32, one)
+        rules.history_len = history_len.data_ptr()
+    if bias_row is not None:
+        _dense(what, "bias_row", bias_row, i32, one)
+        rules.bias_row = bias_row.data_ptr()
+    if mask_row is not None:
+        _dense(what, "mask_row", mask_row, i32, one)
+        rules.mask_row = mask_row.data_ptr()
+    if repetition is not None:
+        _dense(what, "repetition", repetition, f32, one)
+        rules.repetition = repetition.data_ptr()
+    if presence is not None:
+        _dense(what, "presence", presence, f32, one)
+        rules.presence = presence.data_ptr()
+    if frequency is not None:
+        _dense(what, "frequency", frequency, f32, one)
+        rules.frequency = frequency.data_ptr()
+    if out is None:
+        out = torch.empty_like(logits)
+    else:
+        _dense(what, "out", out, dtype, shape)
     L = lib()
-    rules = LogitRules(_ptr(history), _ptr(history_len), 0 if history is None else history.shape[1], _ptr(repetition), _ptr(presence), _ptr(frequency),
-                       _ptr(bias), _ptr(bias_row), 0 if bias is None else bias.shape[0], _ptr(mask), _ptr(mask_row), 0 if mask is None else mask.shape[0])
-    entry = L.gr4ad_op_adjust_logits if logits.dtype == torch.float32 else L.gr4ad_op_adjust_logits_f16
-    with _On(logits.device, stream) as st:
-        if out is None:
-            out = torch.empty_like(logits)
-        _check(entry(logits.data_ptr(), out.data_ptr(), rows, V, C.byref(rules), st))
+    _check((L.gr4ad_op_adjust_logits if dtype is f32 else L.gr4ad_op_adjust_logits_f16)(logits.data_ptr(), out.data_ptr(), rows, V, C.byref(rules), _raw_stream(_device())))
     return out
 
 
