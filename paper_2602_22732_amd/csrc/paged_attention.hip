@@ -10,6 +10,7 @@
 //  * paged_append<T>        new keys and values into their pages.
 //  * paged_rows<T, DH>      16 rows (token, head of the group) of one (sequence, key head) per workgroup, whose wavefronts walk
 //                           stretches of the keys of their own; operands go from memory to registers.
+//  * paged_flash<DH>        128 rows per workgroup, keys and values staged in LDS (bf16).
 //  * paged_join<T, DH>      joins the stretches of several workgroups.
 #include "common.h"
 
@@ -64,6 +65,39 @@ template <typename F> __device__ __forceinline__ bool find_sequence(const PagedA
         before += all;
     }
     return false;
+}
+
+// The same with the longest sequences first (B <= 64), so that their tiles do not start last; otherwise in their order.
+template <typename F> __device__ __forceinline__ bool find_longest_first(const PagedArgs &a, int64_t t, F tiles, Sequence &s) {
+    if (a.B > 64) return find_sequence(a, t, tiles, s);
+    const int lane = threadIdx.x % 64;
+    int start = 0, m = 0, len = -1, count = 0, rank = 0;
+    if (lane < a.B) {
+        start = min(max(a.q_start[lane], 0), a.N);
+        m = min(max(a.q_start[lane + 1], start), a.N) - start;
+        len = min(max(a.seq_len[lane], 0), a.max_pages << a.page_shift);
+        count = tiles(m, len);
+    }
+    for (int i = 0; i < a.B; i++) {
+        const int other = __builtin_amdgcn_readlane(len, i);
+        rank += other > len || (other == len && i < lane) ? 1 : 0;
+    }
+    if (lane >= a.B) rank = lane;
+    auto sorted = [&](int v) { return __builtin_amdgcn_ds_permute(rank * 4, v); };
+    const int b = sorted(lane);
+    start = sorted(start);
+    m = sorted(m);
+    len = sorted(len);
+    count = sorted(count);
+    const int upto = wave_scan(count);
+    if (t >= __builtin_amdgcn_readlane(upto, 63)) return false;
+    const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > t));
+    s.b = __builtin_amdgcn_readlane(b, src);
+    s.start = __builtin_amdgcn_readlane(start, src);
+    s.m = __builtin_amdgcn_readlane(m, src);
+    s.len = __builtin_amdgcn_readlane(len, src);
+    s.tile = (int)t - (__builtin_amdgcn_readlane(upto, src) - __builtin_amdgcn_readlane(count, src));
+    return true;
 }
 
 __device__ __forceinline__ int page_of(const PagedArgs &a, int b, int key) { return a.table[(int64_t)b * a.max_pages + (key >> a.page_shift)]; }
@@ -440,6 +474,210 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void paged_rows(
     }
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// Many rows: 128 rows (token, head of the group) of one (sequence, key head) per workgroup, 32 to a wavefront.  The keys stream through LDS in tiles of 64
+// [64 x DH] with their values [DH x 64], two tiles double-buffered, filled by direct global->LDS loads.  Both products are transposed, so a lane owns
+// one row: its maximum and sum are its own, and P^T leaves the first product as the second's operand (key rows enter with bits 2 and 3 of their index
+// swapped, which makes the eight keys a lane holds for one MFMA step consecutive).
+// ---------------------------------------------------------------------------------------------------------------------
+template <int DH> __global__ __launch_bounds__(256, 2) void paged_flash(PagedArgs a) {
+    constexpr int NW = 4, ROWS = NW * 32, KT = 64, KCH = DH / 8, K_CHUNKS = KT * KCH, STAGE = 2 * K_CHUNKS, KSTEPS = DH / 16, MT = DH / 32, KI = K_CHUNKS / 64 / NW;
+    extern __shared__ bf16x8 smem[];  // 2 * STAGE chunks
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), frow = lane % 32, hf = lane / 32;
+    const int split = blockIdx.x / a.Hkv % a.nsplit, kvh = blockIdx.x % a.Hkv, page = 1 << a.page_shift;
+    Sequence s;
+    if (!find_longest_first(a, blockIdx.x / (a.nsplit * a.Hkv), [&](int m, int) { return (m * a.group + ROWS - 1) / ROWS; }, s)) return;
+    // (the last rows of a sequence see the most keys: first)
+    const int R0 = ((s.m * a.group + ROWS - 1) / ROWS - 1 - s.tile) * ROWS, R1 = min(R0 + ROWS, s.m * a.group), base = s.len - s.m;
+    const int p_lo = base + R0 / a.group, p_hi = base + (R1 - 1) / a.group;
+    const Blocks bl = visible_blocks<KT>(a, p_lo, p_hi);
+    const int each = (bl.count + a.nsplit - 1) / a.nsplit, x0 = min(split * each, bl.count), x1 = min(x0 + each, bl.count);
+
+    const int R = R0 + wave * 32 + frow, tok = R / a.group, head = kvh * a.group + R - tok * a.group, p = R < R1 ? base + tok : -1;
+    bf16x8 qf[KSTEPS];
+    {
+        const bf16 *q = (const bf16 *)a.q + (int64_t)(s.start + min(tok, s.m - 1)) * a.q_stride + head * DH + 8 * hf;
+#pragma unroll
+        for (int st = 0; st < KSTEPS; st++) qf[st] = R < R1 ? *(const bf16x8 *)(q + 16 * st) : bf16x8{};
+    }
+
+    // Page numbers: one of 64 successive pages per lane.  Every wavefront loads its share of a tile, so all keep them.
+    int ids = 0, ids_from = 0;
+    auto want_pages = [&](int x) {  // uniform
+        const int first = bl.at(x) * KT >> a.page_shift, last = (bl.at(x) * KT + KT - 1) >> a.page_shift;
+        if (x == x0 || last >= ids_from + 64) {
+            ids_from = first;
+            const int at = first + lane;
+            ids = at < a.max_pages ? a.table[(int64_t)s.b * a.max_pages + at] : -1;
+        }
+    };
+    auto exists = [&](int id) { return id >= 0 && id < a.n_pages; };
+    auto issue = [&](int x, int buf) {
+        want_pages(x);
+        const int key0 = bl.at(x) * KT, pg0 = (key0 >> a.page_shift) - ids_from;
+        bf16x8 *dst = smem + buf * STAGE;
+#pragma unroll
+        for (int i = 0; i < KI; i++) {  // 64 chunks of K rows: at most 16 rows, on one page
+            const int w = i * NW + wave, r = (w * 64 + lane) / KCH, r0 = w * 64 / KCH;
+            int id = __builtin_amdgcn_readlane(ids, pg0 + (((key0 & (page - 1)) + r0) >> a.page_shift));
+            if (!exists(id)) id = 0;
+            const bf16 *src = (const bf16 *)a.k + (((int64_t)id * a.Hkv + kvh) * page + ((key0 + r0) & (page - 1))) * DH;
+            const int c = ((w * 64 + lane) % KCH) ^ ((KCH >= 8 ? (r >> 1) : (r >> 2)) & (KCH - 1) & 7);
+            __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)(src + (r - r0) * DH + c * 8),
+                                             (void __attribute__((address_space(3))) *)(dst + w * 64), 16, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < KI; i++) {  // eight rows of V^T
+            const int w = i * NW + wave, r = w * 8 + lane / 8, c = (lane % 8) ^ ((r >> 1) & 7), slot = (key0 & (page - 1)) + 8 * c;
+            int id = __builtin_amdgcn_ds_bpermute((pg0 + (slot >> a.page_shift)) * 4, ids);
+            if (!exists(id)) id = 0;
+            const bf16 *src = (const bf16 *)a.v + (((int64_t)id * a.Hkv + kvh) * DH + r) * page + (slot & (page - 1));
+            __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)src, (void __attribute__((address_space(3))) *)(dst + K_CHUNKS + w * 64), 16, 0, 0);
+        }
+    };
+    // bit i: the keys of chunk i of a tile lie on a page that exists and some row of the workgroup may see some of them
+    auto tile_valid = [&](int x) -> unsigned {
+        const int key0 = bl.at(x) * KT, slot = (key0 & (page - 1)) + 8 * (lane % 8);
+        const int id = __builtin_amdgcn_ds_bpermute(((key0 >> a.page_shift) - ids_from + (slot >> a.page_shift)) * 4, ids);
+        return (unsigned)__builtin_amdgcn_ballot_w64(exists(id)) & 0xFFu;
+    };
+
+    float m_run = -INFINITY, l_run = 0.0f;
+    floatx16 o[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) o[mt][v] = 0.0f;
+    const int krow = (frow & 0x13) | ((frow & 4) << 1) | ((frow & 8) >> 1);
+    unsigned valid = 0xFF;
+    if (x0 < x1) {
+        issue(x0, 0);
+        valid = tile_valid(x0);
+    }
+    int buf = 0;
+    for (int x = x0; x < x1; x++) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const unsigned now_valid = valid;
+        if (x + 1 < x1) {
+            issue(x + 1, buf ^ 1);
+            valid = tile_valid(x + 1);
+        }
+        const int key0 = bl.at(x) * KT;
+        bf16x8 *sk = smem + buf * STAGE, *sv = sk + K_CHUNKS;
+        buf ^= 1;
+        if (now_valid != 0xFF || key0 + KT - 1 > p_hi) {
+            // values no row of the workgroup may use: out of the product, where p = 0 would not keep an infinity or a NaN out
+            for (int id = threadIdx.x; id < DH * 8; id += 256) {
+                const int r = id / 8, c = (id % 8) ^ ((r >> 1) & 7);
+                bf16x8 v = sv[id];
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if (!(now_valid >> c & 1) || key0 + 8 * c + e > p_hi) v[e] = (bf16)0.0f;
+                sv[id] = v;
+            }
+            __syncthreads();
+        }
+        if (R0 + wave * 32 >= R1) continue;  // a wavefront without rows
+        floatx16 sc[2];
+#pragma unroll
+        for (int sub = 0; sub < 2; sub++)
+#pragma unroll
+            for (int v = 0; v < 16; v++) sc[sub][v] = 0.0f;
+#pragma unroll
+        for (int st = 0; st < KSTEPS; st++)
+#pragma unroll
+            for (int sub = 0; sub < 2; sub++) {
+                const int r = sub * 32 + krow;
+                const bf16x8 kf = sk[r * KCH + ((2 * st + hf) ^ ((KCH >= 8 ? (r >> 1) : (r >> 2)) & (KCH - 1) & 7))];
+                sc[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], sc[sub], 0, 0, 0);
+            }
+        // this lane holds, for its row, keys key0 + 32 sub + 16 (v / 8) + 8 hf + v % 8
+        if (now_valid != 0xFF || key0 + KT - 1 > p_lo || (a.window && p_hi - key0 >= a.window && key0 + KT > a.sinks)) {
+#pragma unroll
+            for (int sub = 0; sub < 2; sub++)
+#pragma unroll
+                for (int v = 0; v < 16; v++) {
+                    const int kk = 32 * sub + 16 * (v / 8) + 8 * hf + v % 8;
+                    if (!sees(a, p, key0 + kk) || !(now_valid >> (kk / 8) & 1)) sc[sub][v] = -INFINITY;
+                }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int sub = 0; sub < 2; sub++)
+#pragma unroll
+            for (int v = 0; v < 16; v++) mx = fmaxf(mx, sc[sub][v]);
+        mx = halves_max(mx) * a.scale_log2e;
+        if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0) {  // some row outgrew the maximum it uses by 2^8
+            const float mn = mx > m_run + 8.0f ? mx : m_run, alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - mn);
+            m_run = mn;
+            l_run *= alpha;
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+                for (int v = 0; v < 16; v++) o[mt][v] *= alpha;
+        }
+        const float neg = m_run == -INFINITY ? 0.0f : -m_run;
+        bf16x8 pf[4];  // (weights rounded once, as the operand of the matrix instruction; the normaliser adds them unrounded)
+        float lsum = 0.0f;
+#pragma unroll
+        for (int sub = 0; sub < 2; sub++)
+#pragma unroll
+            for (int v = 0; v < 16; v++) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][v], a.scale_log2e, neg));
+                lsum += w;
+                pf[2 * sub + v / 8][v % 8] = (bf16)w;
+            }
+        l_run += lsum;
+#pragma unroll
+        for (int ks = 0; ks < 4; ks++)
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++) {
+                const int r = mt * 32 + frow;
+                const bf16x8 vf = sv[r * 8 + ((2 * ks + hf) ^ ((r >> 1) & 7))];
+                o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[ks], o[mt], 0, 0, 0);
+            }
+    }
+    const float l = halves_sum(l_run);
+    bool bad = !(l < INFINITY);
+#pragma unroll
+    for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) bad |= !(fabsf(o[mt][v]) < INFINITY);
+    const int row = s.start + tok;
+    if (R < R1) {
+        if (a.nsplit > 1) {
+            float *part = part_row<DH>(a, row, head, split);
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+                for (int v = 0; v < 16; v++) part[mt * 32 + 8 * (v / 4) + 4 * hf + v % 4] = o[mt][v];
+            if (hf == 0) {
+                part[DH] = m_run;
+                part[DH + 1] = l;
+            }
+        } else {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            bf16 *dst = out_row<bf16, DH>(a, row, head);
+#pragma unroll
+            for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+                for (int g = 0; g < 4; g++) {
+                    bf16x4 pk;
+#pragma unroll
+                    for (int j = 0; j < 4; j++) pk[j] = (bf16)(o[mt][4 * g + j] * inv);
+                    *(bf16x4 *)(dst + mt * 32 + 8 * g + 4 * hf) = pk;
+                }
+        }
+    }
+    if (__builtin_amdgcn_ballot_w64(bad && R < R1) != 0)
+        for (int i = 0; i < 32 && R0 + wave * 32 + i < R1; i++) {
+            const int RR = R0 + wave * 32 + i, tk = RR / a.group;
+            plain_row<bf16, DH, KT>(a, s, bl, x0, x1, kvh, s.start + tk, kvh * a.group + RR - tk * a.group, base + tk, split);
+        }
+}
+
 // Joins the workgroups' shares of a row: one wavefront per row.
 template <typename T, int DH> __global__ __launch_bounds__(256) void paged_join(PagedArgs a) {
     const int lane = threadIdx.x % 64;
@@ -475,29 +713,37 @@ int shift_of(int page) {
     return s;
 }
 
-// Stretches of the keys that workgroups of their own walk.
-int splits_of(int64_t tiles, int Hkv, int64_t most_keys) {
-    const int64_t want = (2048 + tiles * Hkv - 1) / (tiles * Hkv), most = (most_keys + 255) / 256;
-    const int64_t n = want < most ? want : most;
-    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+constexpr int kFlashRows = 128;
+
+// bound of the tiles of `rows` rows, of one key head
+int64_t tiles_of(int N, int B, int group, int rows) {
+    const int64_t all = (int64_t)N * group, n = all / rows + B;
+    return n < all ? n : all;
 }
 
-struct Plan { int64_t tiles; int nsplit; size_t bytes; };
-Plan plan_of(int B, int N, int H, int Hkv, int dh, int page, int max_pages, int window, int sinks) {
+// flash: tiles of 128 rows share the staged keys; otherwise 16 rows.  nsplit: workgroups that share a tile's keys.
+struct Plan { bool flash; int64_t tiles; int nsplit; size_t bytes; };
+Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, int max_pages, int window, int sinks) {
     Plan p;
-    p.tiles = (int64_t)N * (H / Hkv) / kRows + B;
-    if (p.tiles > (int64_t)N * (H / Hkv)) p.tiles = (int64_t)N * (H / Hkv);
+    const int group = H / Hkv;
+    p.flash = dtype == GR4AD_BF16 && dh >= 32 && (int64_t)N * group >= 64 * (int64_t)B;
+    p.tiles = tiles_of(N, B, group, kRows);
+    const int64_t blocks = (p.flash ? tiles_of(N, B, group, kFlashRows) : p.tiles) * Hkv, enough = p.flash ? 512 : 2048, least = p.flash ? 1024 : 256;
     int64_t keys = (int64_t)max_pages * page;
     if (window && (int64_t)window + sinks + 64 < keys) keys = (int64_t)window + sinks + 64;
-    p.nsplit = splits_of(p.tiles, Hkv, keys);
+    const int64_t want = (enough + blocks - 1) / blocks, most = (keys + least - 1) / least, n = want < most ? want : most;
+    p.nsplit = (int)(n < 1 ? 1 : n > 64 ? 64 : n);
     p.bytes = p.nsplit > 1 ? (size_t)N * H * p.nsplit * (dh + 2) * sizeof(float) : 0;
     return p;
 }
 
-template <typename T, int DH> int launch_rows(const PagedArgs &a, hipStream_t st) {
-    const int64_t grid = a.tiles * a.Hkv * a.nsplit;
+template <typename T, int DH> int launch_rows(const PagedArgs &a, bool flash, hipStream_t st) {
+    const int64_t grid = (flash ? tiles_of(a.N, a.B, a.group, kFlashRows) : a.tiles) * a.Hkv * a.nsplit;
     if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
-    hipLaunchKernelGGL((paged_rows<T, DH>), dim3((unsigned)grid), dim3(256), 0, st, a);
+    if constexpr (sizeof(T) == 2 && DH >= 32) {
+        if (flash) hipLaunchKernelGGL((paged_flash<DH>), dim3((unsigned)grid), dim3(256), 64 * DH * 8, st, a);
+    }
+    if (!flash) hipLaunchKernelGGL((paged_rows<T, DH>), dim3((unsigned)grid), dim3(256), 0, st, a);
     GR4AD_LAUNCH_CHECK();
     if (a.nsplit > 1) {
         hipLaunchKernelGGL((paged_join<T, DH>), dim3((unsigned)(a.tiles * a.Hkv * kRows / 4)), dim3(256), 0, st, a);
@@ -505,12 +751,12 @@ template <typename T, int DH> int launch_rows(const PagedArgs &a, hipStream_t st
     }
     return GR4AD_OK;
 }
-template <typename T> int launch_width(const PagedArgs &a, int dh, hipStream_t st) {
+template <typename T> int launch_width(const PagedArgs &a, int dh, bool flash, hipStream_t st) {
     switch (dh) {
-        case 16: return launch_rows<T, 16>(a, st);
-        case 32: return launch_rows<T, 32>(a, st);
-        case 64: return launch_rows<T, 64>(a, st);
-        default: return launch_rows<T, 128>(a, st);
+        case 16: return launch_rows<T, 16>(a, flash, st);
+        case 32: return launch_rows<T, 32>(a, flash, st);
+        case 64: return launch_rows<T, 64>(a, flash, st);
+        default: return launch_rows<T, 128>(a, flash, st);
     }
 }
 
@@ -538,7 +784,7 @@ extern "C" {
 
 size_t gr4ad_op_paged_attention_workspace_bytes(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, int32_t B, int32_t N, int32_t H, int32_t window, int32_t sinks) {
     if (check_shape(dtype, cache, B, N, H, window, sinks)) return 0;
-    return plan_of(B, N, H, cache->H_kv, cache->dh, cache->page_size, cache->max_pages, window, sinks).bytes;
+    return plan_of(dtype, B, N, H, cache->H_kv, cache->dh, cache->page_size, cache->max_pages, window, sinks).bytes;
 }
 
 int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, const void *q, int64_t q_stride, const void *k_new, const void *v_new, int64_t kv_stride,
@@ -554,7 +800,7 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
     if (q_stride < (int64_t)H * c.dh || (k_new && kv_stride < (int64_t)c.H_kv * c.dh)) return gr4ad_set_thread_error(GR4AD_EINVAL, "paged attention: rows overlap (strides in elements)");
     if (q_stride % piece || kv_stride % piece || (uintptr_t)k_new % 16 || (uintptr_t)v_new % 16 || (uintptr_t)q % 16 || (uintptr_t)c.k_pages % 16 || (uintptr_t)c.v_pages % 16 || (uintptr_t)out % 16)
         return gr4ad_set_thread_error(GR4AD_EINVAL, "paged attention: q, k_new, v_new, their rows, the pages and out must be 16-byte aligned");
-    const Plan p = plan_of(B, N, H, c.H_kv, c.dh, c.page_size, c.max_pages, window, sinks);
+    const Plan p = plan_of(dtype, B, N, H, c.H_kv, c.dh, c.page_size, c.max_pages, window, sinks);
     if (p.bytes && (!workspace || workspace_bytes < p.bytes || (uintptr_t)workspace % 16))
         return gr4ad_set_thread_error(GR4AD_EWORKSPACE, "paged attention: workspace of %zu bytes needed, 16-byte aligned", p.bytes);
     hipStream_t st = (hipStream_t)hip_stream;
@@ -574,7 +820,7 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
     // lengths lie on the device: counted on all pages of every sequence, an upper bound
     const double keys = (double)c.max_pages * c.page_size;
     ProfScope ps(KC_PAGED_ATTN, st, 4.0 * N * keys * H * c.dh, e * (2.0 * B * keys * c.H_kv * c.dh + 2.0 * N * H * c.dh));
-    return dtype == GR4AD_BF16 ? launch_width<bf16>(a, c.dh, st) : launch_width<float>(a, c.dh, st);
+    return dtype == GR4AD_BF16 ? launch_width<bf16>(a, c.dh, p.flash, st) : launch_width<float>(a, c.dh, false, st);
 }
 
 }  // extern "C"
