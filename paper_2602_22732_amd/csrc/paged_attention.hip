@@ -12,6 +12,8 @@
 //                           stretches of the keys of their own; operands go from memory to registers.
 //  * paged_flash<DH>        128 rows per workgroup, keys and values staged in LDS (bf16).
 //  * paged_join<T, DH>      joins the stretches of several workgroups.
+#include <type_traits>
+
 #include "common.h"
 
 namespace {
@@ -201,6 +203,25 @@ __device__ void plain_row(const PagedArgs &a, const Sequence &s, const Blocks &b
     }
 }
 
+// The kernel's arguments, read again where this stands: what only the rare path needs does not occupy scalar registers before it.
+__device__ __forceinline__ PagedArgs late_args() {
+    const __attribute__((address_space(4))) char *at = (const __attribute__((address_space(4))) char *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    PagedArgs a;
+    __builtin_memcpy(&a, (const char *)at, sizeof(a));
+    return a;
+}
+
+// Numbers of 64 successive pages of sequence b from `first` on, one per lane; -1 past the table.  Load and wait in one: a load that the compiler tracks
+// would have every later use of the numbers wait for all keys and values on their way.
+__device__ __forceinline__ int page_numbers(const PagedArgs &a, int b, int first) {
+    const int at = first + threadIdx.x % 64;
+    const int32_t *src = a.table + (int64_t)b * a.max_pages + min(at, a.max_pages - 1);
+    int id;
+    asm volatile("global_load_dword %0, %1, off\n\ts_waitcnt vmcnt(0)" : "=&v"(id) : "v"(src) : "memory");
+    return at < a.max_pages ? id : -1;
+}
+
 // Fragments of one block of keys as the two products take them.  bf16: v_mfma_f32_16x16x32_bf16, 32 keys; float32: v_mfma_f32_16x16x4_f32, 16 keys.
 // A lane holds row lane % 16 of the first operand and c = lane / 16 says which part of the contraction; of S^T it gets query lane % 16 and four rows.
 // bf16: key rows enter in an order that makes the eight keys a lane then holds of P consecutive, as its piece of V^T has them.
@@ -247,11 +268,18 @@ template <int DH> struct Frags<bf16, DH> {
         }
     }
     __device__ __forceinline__ void add_values(floatx4 (&o)[VF], const floatx4 (&p)[2]) const {
-        bf16x8 w;  // (rounded once, as the operand of the matrix instruction; the normaliser adds the unrounded terms)
+        // A weight as the sum of two bf16 numbers, 16 bits of it: the second product costs nothing where memory is what bounds, and the result then carries
+        // one rounding, its own (with one product of rounded weights it is off by 0.0022 to 0.0023 of its norm, with two by 0.0017, as a float32 form is).
+        bf16x8 w, rest;
 #pragma unroll
-        for (int e = 0; e < 8; e++) w[e] = (bf16)p[e / 4][e % 4];
+        for (int e = 0; e < 8; e++) {
+            w[e] = (bf16)p[e / 4][e % 4];
+            rest[e] = (bf16)(p[e / 4][e % 4] - (float)w[e]);
+        }
 #pragma unroll
         for (int t = 0; t < VF; t++) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], w, o[t], 0, 0, 0);
+#pragma unroll
+        for (int t = 0; t < VF; t++) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], rest, o[t], 0, 0, 0);
     }
     // values of keys nobody in the tile may use (slots behind the last token): out of the product
     __device__ __forceinline__ void drop_values(int from) {
@@ -343,27 +371,32 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void paged_rows(
 
     // page numbers: one of 64 successive pages per lane
     int ids = 0, ids_from = -64;
-    auto page_id = [&](int pg) {
-        if (pg < ids_from || pg >= ids_from + 64) {
+    auto page_id = [&](int key) {
+        const int pg = key >> a.page_shift;
+        if (pg >= ids_from + 64) {
             ids_from = pg;
-            const int at = pg + lane;
-            ids = at < a.max_pages ? a.table[(int64_t)s.b * a.max_pages + at] : -1;
+            ids = page_numbers(a, s.b, pg);
         }
         return __builtin_amdgcn_readlane(ids, pg - ids_from);
     };
     struct Source { const T *k[2], *v[2]; int valid; };  // valid: bit i: keys 16 i .. 16 i + 15 of the block lie on a page that exists
     auto source = [&](int x) {
         Source r;
-        r.valid = 0;
-#pragma unroll
-        for (int i = 0; i < 2; i++) {
-            const int key = bl.at(x) * KB + (KB == 32 ? 16 * i : 0), slot = key & (page - 1);
-            int id = (key >> a.page_shift) < a.max_pages ? page_id(key >> a.page_shift) : -1;
-            if (id >= 0 && id < a.n_pages) r.valid |= 1 << i;
-            else id = 0;
-            const int64_t hd = (int64_t)id * a.Hkv + kvh;
-            r.k[i] = (const T *)a.k + (hd * page + slot) * DH;
-            r.v[i] = (const T *)a.v + hd * DH * page + slot;
+        const int key = bl.at(x) * KB, id = page_id(key), slot = key & (page - 1);
+        const bool there = id >= 0 && id < a.n_pages;
+        const int64_t hd = (int64_t)(there ? id : 0) * a.Hkv + kvh;
+        r.valid = there ? 3 : 0;
+        r.k[0] = (const T *)a.k + (hd * page + slot) * DH;
+        r.v[0] = (const T *)a.v + hd * DH * page + slot;
+        r.k[1] = r.k[0] + 16 * DH;
+        r.v[1] = r.v[0] + 16;
+        if (KB == 32 && page == 16) {  // the block's second half lies on the next page
+            const int id1 = page_id(key + 16);
+            const bool there1 = id1 >= 0 && id1 < a.n_pages;
+            const int64_t hd1 = (int64_t)(there1 ? id1 : 0) * a.Hkv + kvh;
+            r.valid = (there ? 1 : 0) | (there1 ? 2 : 0);
+            r.k[1] = (const T *)a.k + hd1 * page * DH;
+            r.v[1] = (const T *)a.v + hd1 * DH * page;
         }
         return r;
     };
@@ -429,6 +462,7 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void paged_rows(
     l_run = query_sum(l_run);
 
     // the wavefronts' stretches, joined in their order
+    const PagedArgs z = late_args();
     __shared__ float sm[NW][kRows], sl[NW][kRows];
     __shared__ __attribute__((aligned(16))) float so[NW][kRows][DH + 4];
     if (c == 0) {
@@ -453,36 +487,39 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void paged_rows(
             v = fmaf(so[w][r][d], f_, v);
             bad |= !(fabsf(so[w][r][d]) < INFINITY) || !(sl[w][r] < INFINITY);
         }
-        const int tk = RR / a.group, row = s.start + tk, hd = kvh * a.group + RR - tk * a.group;
-        if (a.nsplit > 1) {
-            float *part = part_row<DH>(a, row, hd, split);
+        const int tk = RR / z.group, row = s.start + tk, hd = kvh * z.group + RR - tk * z.group;
+        if (z.nsplit > 1) {
+            float *part = part_row<DH>(z, row, hd, split);
             part[d] = v;
             if (d == 0) {
                 part[DH] = m;
                 part[DH + 1] = l;
             }
         } else {
-            out_row<T, DH>(a, row, hd)[d] = from_f<T>(l == 0.0f ? 0.0f : v / l);
+            out_row<T, DH>(z, row, hd)[d] = from_f<T>(l == 0.0f ? 0.0f : v / l);
         }
     }
     if (__syncthreads_or(bad)) {
         const int y0 = min(split * NW * each, bl.count), y1 = min(y0 + NW * each, bl.count);
         for (int r = wave; r < R1 - R0; r += NW) {
-            const int RR = R0 + r, tk = RR / a.group;
-            plain_row<T, DH, KB>(a, s, bl, y0, y1, kvh, s.start + tk, kvh * a.group + RR - tk * a.group, base + tk, split);
+            const int RR = R0 + r, tk = RR / z.group;
+            plain_row<T, DH, KB>(z, s, bl, y0, y1, kvh, s.start + tk, kvh * z.group + RR - tk * z.group, base + tk, split);
         }
     }
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Many rows: 128 rows (token, head of the group) of one (sequence, key head) per workgroup, 32 to a wavefront.  The keys stream through LDS in tiles of 64
-// [64 x DH] with their values [DH x 64], two tiles double-buffered, filled by direct global->LDS loads.  Both products are transposed, so a lane owns
-// one row: its maximum and sum are its own, and P^T leaves the first product as the second's operand (key rows enter with bits 2 and 3 of their index
+// Many rows: QB * 128 rows (token, head of the group) of one (sequence, key head) per workgroup, QB * 32 to a wavefront.  The keys stream through LDS in
+// tiles of 64 [64 x DH] with their values [DH x 64], two of each, filled by direct global->LDS loads.  Both products are transposed, so a lane owns
+// QB rows: their maxima and sums are its own, and P^T leaves the first product as the second's operand (key rows enter with bits 2 and 3 of their index
 // swapped, which makes the eight keys a lane holds for one MFMA step consecutive).
+// The matrix cores and the vector instructions of the softmax need about the same time, so a wavefront runs them side by side: the scores of tile x + 1 are
+// formed while those of tile x become weights, and the maximum of tile x + 1 is found while the values of tile x are added.  QB = 2: a fragment read from
+// LDS feeds two MFMAs (with one, 32 KB of LDS reads per wavefront and tile take as long as the MFMAs).
 // ---------------------------------------------------------------------------------------------------------------------
-template <int DH> __global__ __launch_bounds__(256, 2) void paged_flash(PagedArgs a) {
-    constexpr int NW = 4, ROWS = NW * 32, KT = 64, KCH = DH / 8, K_CHUNKS = KT * KCH, STAGE = 2 * K_CHUNKS, KSTEPS = DH / 16, MT = DH / 32, KI = K_CHUNKS / 64 / NW;
-    extern __shared__ bf16x8 smem[];  // 2 * STAGE chunks
+template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) void paged_flash(PagedArgs a) {
+    constexpr int QB = 1, ROWS = NW * 32 * QB, KT = 64, KCH = DH / 8, HALF = KT * KCH, KSTEPS = DH / 16, MT = DH / 32, KI = HALF / 64 / NW, LEAD = SLOTS - 1;
+    extern __shared__ bf16x8 smem[];  // keys of SLOTS tiles, values of SLOTS tiles: HALF chunks each
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), frow = lane % 32, hf = lane / 32;
     const int split = blockIdx.x / a.Hkv % a.nsplit, kvh = blockIdx.x % a.Hkv, page = 1 << a.page_shift;
     Sequence s;
@@ -493,12 +530,17 @@ template <int DH> __global__ __launch_bounds__(256, 2) void paged_flash(PagedArg
     const Blocks bl = visible_blocks<KT>(a, p_lo, p_hi);
     const int each = (bl.count + a.nsplit - 1) / a.nsplit, x0 = min(split * each, bl.count), x1 = min(x0 + each, bl.count);
 
-    const int R = R0 + wave * 32 + frow, tok = R / a.group, head = kvh * a.group + R - tok * a.group, p = R < R1 ? base + tok : -1;
-    bf16x8 qf[KSTEPS];
-    {
+    const int W0 = R0 + wave * 32 * QB;  // the wavefront's first row
+    int p[QB];
+    bf16x8 qf[QB][KSTEPS];
+#pragma unroll
+    for (int i = 0; i < QB; i++) {
+        const int R = W0 + 32 * i + frow, tok = R / a.group, head = kvh * a.group + R - tok * a.group;
+        p[i] = R < R1 ? base + tok : -1;
+        // (rows past the last repeat a token's: they are computed and dropped)
         const bf16 *q = (const bf16 *)a.q + (int64_t)(s.start + min(tok, s.m - 1)) * a.q_stride + head * DH + 8 * hf;
 #pragma unroll
-        for (int st = 0; st < KSTEPS; st++) qf[st] = R < R1 ? *(const bf16x8 *)(q + 16 * st) : bf16x8{};
+        for (int st = 0; st < KSTEPS; st++) qf[i][st] = *(const bf16x8 *)(q + 16 * st);
     }
 
     // Page numbers: one of 64 successive pages per lane.  Every wavefront loads its share of a tile, so all keep them.
@@ -507,174 +549,371 @@ template <int DH> __global__ __launch_bounds__(256, 2) void paged_flash(PagedArg
         const int first = bl.at(x) * KT >> a.page_shift, last = (bl.at(x) * KT + KT - 1) >> a.page_shift;
         if (x == x0 || last >= ids_from + 64) {
             ids_from = first;
-            const int at = first + lane;
-            ids = at < a.max_pages ? a.table[(int64_t)s.b * a.max_pages + at] : -1;
+            ids = page_numbers(a, s.b, first);
         }
     };
     auto exists = [&](int id) { return id >= 0 && id < a.n_pages; };
-    auto issue = [&](int x, int buf) {
-        want_pages(x);
-        const int key0 = bl.at(x) * KT, pg0 = (key0 >> a.page_shift) - ids_from;
-        bf16x8 *dst = smem + buf * STAGE;
+    // A lane's place in a load of 64 chunks does not depend on which of its loads it is: chunk c of row r lies at c ^ swizzle(r)
+    constexpr int KR = 64 / KCH;  // rows of K per load
+    auto swizzle = [](int r) { return KCH == 16 ? r & 15 : KCH == 8 ? (r >> 1) & 7 : (r >> 2) & 3; };  // 16 successive rows' same chunk: 256 bytes of LDS, all banks once
+    const int k_row = lane / KCH, k_swz = swizzle(wave * KR + k_row);
+    const unsigned k_off = (unsigned)(k_row * DH + (((lane % KCH) ^ k_swz) * 8));
+    const int v_row = wave * 8 + lane / 8, v_chunk = (lane % 8) ^ ((v_row >> 1) & 7);
+    const unsigned v_off = (unsigned)(v_row * page + 8 * v_chunk);
+    auto dma = [&](const bf16 *src, bf16x8 *dst) {
+        __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)src, (void __attribute__((address_space(3))) *)dst, 16, 0, 0);
+    };
+    // A tile on one page (page_size >= 64): where this head's part of the page begins, and whether the page exists (otherwise page 0 is loaded and masked)
+    auto page_start = [&](int x, bool &there) {
+        const int id = __builtin_amdgcn_readlane(ids, (bl.at(x) * KT >> a.page_shift) - ids_from);
+        there = exists(id);
+        return ((int64_t)(there ? id : 0) * a.Hkv + kvh) * (DH << a.page_shift);
+    };
+    auto issue_k_at = [&](int64_t start, int slot0, int buf) {
+        const bf16 *src = (const bf16 *)a.k + start + (slot0 + wave * KR) * DH;
+        bf16x8 *dst = smem + buf * HALF + wave * 64;
 #pragma unroll
-        for (int i = 0; i < KI; i++) {  // 64 chunks of K rows: at most 16 rows, on one page
-            const int w = i * NW + wave, r = (w * 64 + lane) / KCH, r0 = w * 64 / KCH;
-            int id = __builtin_amdgcn_readlane(ids, pg0 + (((key0 & (page - 1)) + r0) >> a.page_shift));
-            if (!exists(id)) id = 0;
-            const bf16 *src = (const bf16 *)a.k + (((int64_t)id * a.Hkv + kvh) * page + ((key0 + r0) & (page - 1))) * DH;
-            const int c = ((w * 64 + lane) % KCH) ^ ((KCH >= 8 ? (r >> 1) : (r >> 2)) & (KCH - 1) & 7);
-            __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)(src + (r - r0) * DH + c * 8),
-                                             (void __attribute__((address_space(3))) *)(dst + w * 64), 16, 0, 0);
-        }
+        for (int i = 0; i < KI; i++) dma(src + i * NW * KR * DH + k_off, dst + i * NW * 64);
+    };
+    auto issue_v_at = [&](int64_t start, int slot0, int buf) {
+        const bf16 *src = (const bf16 *)a.v + start + slot0;
+        bf16x8 *dst = smem + (SLOTS + buf) * HALF + wave * 64;
 #pragma unroll
-        for (int i = 0; i < KI; i++) {  // eight rows of V^T
-            const int w = i * NW + wave, r = w * 8 + lane / 8, c = (lane % 8) ^ ((r >> 1) & 7), slot = (key0 & (page - 1)) + 8 * c;
-            int id = __builtin_amdgcn_ds_bpermute((pg0 + (slot >> a.page_shift)) * 4, ids);
-            if (!exists(id)) id = 0;
-            const bf16 *src = (const bf16 *)a.v + (((int64_t)id * a.Hkv + kvh) * DH + r) * page + (slot & (page - 1));
-            __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)src, (void __attribute__((address_space(3))) *)(dst + K_CHUNKS + w * 64), 16, 0, 0);
+        for (int i = 0; i < KI; i++) dma(src + i * NW * 8 * page + v_off, dst + i * NW * 64);
+    };
+    // Tiles on several small pages: a page per load of keys (at most 16 rows each), a page per lane for the values
+    auto issue_k_small = [&](int x, int buf) {
+        const int key0 = bl.at(x) * KT, slot0 = key0 & (page - 1), pg0 = (key0 >> a.page_shift) - ids_from;
+        bf16x8 *dst = smem + buf * HALF + wave * 64;
+#pragma unroll
+        for (int i = 0; i < KI; i++) {
+            const int slot = slot0 + (i * NW + wave) * KR, id = __builtin_amdgcn_readlane(ids, pg0 + (slot >> a.page_shift));
+            dma((const bf16 *)a.k + (((int64_t)(exists(id) ? id : 0) * a.Hkv + kvh) * page + (slot & (page - 1))) * DH + k_off, dst + i * NW * 64);
         }
     };
-    // bit i: the keys of chunk i of a tile lie on a page that exists and some row of the workgroup may see some of them
-    auto tile_valid = [&](int x) -> unsigned {
+    auto issue_v_small = [&](int x, int buf) {
+        const int key0 = bl.at(x) * KT, slot = (key0 & (page - 1)) + 8 * v_chunk, pg = (key0 >> a.page_shift) - ids_from;
+        const int id = __builtin_amdgcn_ds_bpermute((pg + (slot >> a.page_shift)) * 4, ids);
+        const bf16 *src = (const bf16 *)a.v + (((int64_t)(exists(id) ? id : 0) * a.Hkv + kvh) * DH + v_row) * page + (slot & (page - 1));
+        bf16x8 *dst = smem + (SLOTS + buf) * HALF + wave * 64;
+#pragma unroll
+        for (int i = 0; i < KI; i++) dma(src + i * NW * 8 * page, dst + i * NW * 64);
+    };
+    // bit i: chunk i of a tile's keys lies on a page that exists
+    auto valid_small = [&](int x) -> unsigned {
         const int key0 = bl.at(x) * KT, slot = (key0 & (page - 1)) + 8 * (lane % 8);
         const int id = __builtin_amdgcn_ds_bpermute(((key0 >> a.page_shift) - ids_from + (slot >> a.page_shift)) * 4, ids);
         return (unsigned)__builtin_amdgcn_ballot_w64(exists(id)) & 0xFFu;
     };
 
-    float m_run = -INFINITY, l_run = 0.0f;
-    floatx16 o[MT];
+    float m_run[QB], l_run[QB];
+    floatx16 o[QB][MT];
 #pragma unroll
-    for (int mt = 0; mt < MT; mt++)
+    for (int i = 0; i < QB; i++) {
+        m_run[i] = -INFINITY;
+        l_run[i] = 0.0f;
 #pragma unroll
-        for (int v = 0; v < 16; v++) o[mt][v] = 0.0f;
-    const int krow = (frow & 0x13) | ((frow & 4) << 1) | ((frow & 8) >> 1);
-    unsigned valid = 0xFF;
-    if (x0 < x1) {
-        issue(x0, 0);
-        valid = tile_valid(x0);
+        for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+            for (int v = 0; v < 16; v++) o[i][mt][v] = 0.0f;
     }
-    int buf = 0;
-    for (int x = x0; x < x1; x++) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        const unsigned now_valid = valid;
-        if (x + 1 < x1) {
-            issue(x + 1, buf ^ 1);
-            valid = tile_valid(x + 1);
+    // Fragments by their LDS address: chunk c of row r lies at c ^ swizzle(r), and c = 2 step + hf, so a step flips bits above the lane's own address; the
+    // address is made anew for every tile (kept for every step it costs registers that spill).
+    typedef const __attribute__((address_space(3))) bf16x8 *LdsChunk;
+    const int krow = (frow & 0x13) | ((frow & 4) << 1) | ((frow & 8) >> 1);
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const unsigned k_lane = lds0 + (unsigned)(krow * KCH + (hf ^ swizzle(krow))) * 16, v_lane = lds0 + SLOTS * HALF * 16 + (unsigned)(frow * 8 + (hf ^ ((frow >> 1) & 7))) * 16;
+    auto at_tile = [&](unsigned lane_address, int buf) {
+        unsigned r = lane_address + (unsigned)buf * (HALF * 16);
+        asm volatile("" : "+v"(r));
+        return r;
+    };
+    auto key_frag = [&](unsigned k, int sub, int st) { return *((LdsChunk)(k ^ (unsigned)(st << 5)) + sub * 32 * KCH); };
+    auto value_frag = [&](unsigned v, int ks, int mt) { return *((LdsChunk)(v ^ (unsigned)(ks << 5)) + mt * 256); };
+    struct Scores { floatx16 s[QB][2]; };  // a lane holds, of its row, keys 32 sub + 16 (v / 8) + 8 hf + v % 8
+    bf16x8 pf[QB][4];  // weights, rounded once as the operand of the matrix instruction (the normaliser adds them unrounded)
+    float neg[QB];     // minus the maximum in use
+    // two weights of row i, keys 2 j and 2 j + 1 of the lane's 32, in two parts: the exponentials, and (a step later, when they are there) their sum and rounding
+    auto weigh = [&](Scores &c, int u) {
+        const int i = u % QB, k = 2 * (u / QB);
+#pragma unroll
+        for (int e = k; e < k + 2; e++) {
+            float w = __builtin_amdgcn_exp2f(__builtin_fmaf(c.s[i][e / 16][e % 16], a.scale_log2e, neg[i]));
+            asm volatile("" : "+v"(w));  // (formed here, beside the matrix instructions, and not in the later block that uses it)
+            c.s[i][e / 16][e % 16] = w;
         }
-        const int key0 = bl.at(x) * KT;
-        bf16x8 *sk = smem + buf * STAGE, *sv = sk + K_CHUNKS;
-        buf ^= 1;
-        if (now_valid != 0xFF || key0 + KT - 1 > p_hi) {
-            // values no row of the workgroup may use: out of the product, where p = 0 would not keep an infinity or a NaN out
-            for (int id = threadIdx.x; id < DH * 8; id += 256) {
-                const int r = id / 8, c = (id % 8) ^ ((r >> 1) & 7);
-                bf16x8 v = sv[id];
+    };
+    auto settle = [&](const Scores &c, int u) {
+        const int i = u % QB, k = 2 * (u / QB);
 #pragma unroll
-                for (int e = 0; e < 8; e++)
-                    if (!(now_valid >> c & 1) || key0 + 8 * c + e > p_hi) v[e] = (bf16)0.0f;
-                sv[id] = v;
-            }
-            __syncthreads();
+        for (int e = k; e < k + 2; e++) {
+            const float w = c.s[i][e / 16][e % 16];
+            l_run[i] += w;
+            pf[i][e / 8][e % 8] = (bf16)w;
         }
-        if (R0 + wave * 32 >= R1) continue;  // a wavefront without rows
-        floatx16 sc[2];
+        asm volatile("" : "+v"(l_run[i]));
+        if (k % 8 == 6) asm volatile("" : "+v"(pf[i][k / 8]));
+    };
+    auto weights_upto = [&](Scores &c, int u0, int u1) {
 #pragma unroll
-        for (int sub = 0; sub < 2; sub++)
+        for (int u = u0; u < u1; u++) {
+            weigh(c, u);
+            if (u > 0) settle(c, u - 1);
+        }
+    };
+#define SB __builtin_amdgcn_sched_barrier(0)
+    constexpr int AHEAD = 4;
+    constexpr int PAIRS = 16 * QB, UNDER_SCORES = 12 * QB;  // pairs of weights of a tile; those formed under the next tile's first product
+    // scores of a tile into n, beside the weights of the tile in c (WEIGH; without NEXT the weights alone).  The two halves of the keys in turn, so that the
+    // weights have left half of c's registers before the second half of n needs its own.
+    auto scores = [&](auto next, auto weights, unsigned sk, Scores &n, Scores &c) {
+        constexpr bool NEXT = decltype(next)::value, WEIGH = decltype(weights)::value;
+        constexpr int MM = 2 * KSTEPS * QB;
+        bf16x8 kf[AHEAD];  // fragments are read AHEAD - 1 steps before their MFMAs: the LDS answers in the time of several
+        if constexpr (NEXT) {
 #pragma unroll
-            for (int v = 0; v < 16; v++) sc[sub][v] = 0.0f;
+            for (int f = 0; f < AHEAD - 1; f++) kf[f] = key_frag(sk, f / KSTEPS, f % KSTEPS);
+        }
 #pragma unroll
-        for (int st = 0; st < KSTEPS; st++)
+        for (int sub = 0; sub < 2; sub++) {
+            if constexpr (NEXT) {
 #pragma unroll
-            for (int sub = 0; sub < 2; sub++) {
-                const int r = sub * 32 + krow;
-                const bf16x8 kf = sk[r * KCH + ((2 * st + hf) ^ ((KCH >= 8 ? (r >> 1) : (r >> 2)) & (KCH - 1) & 7))];
-                sc[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[st], sc[sub], 0, 0, 0);
+                for (int i = 0; i < QB; i++)
+#pragma unroll
+                    for (int v = 0; v < 16; v++) n.s[i][sub][v] = 0.0f;
             }
-        // this lane holds, for its row, keys key0 + 32 sub + 16 (v / 8) + 8 hf + v % 8
-        if (now_valid != 0xFF || key0 + KT - 1 > p_lo || (a.window && p_hi - key0 >= a.window && key0 + KT > a.sinks)) {
 #pragma unroll
-            for (int sub = 0; sub < 2; sub++)
+            for (int st = 0; st < KSTEPS; st++) {
+                const int f = sub * KSTEPS + st, ahead = f + AHEAD - 1;
+                if constexpr (NEXT)
+                    if (ahead < 2 * KSTEPS) kf[ahead % AHEAD] = key_frag(sk, ahead / KSTEPS, ahead % KSTEPS);
 #pragma unroll
-                for (int v = 0; v < 16; v++) {
-                    const int kk = 32 * sub + 16 * (v / 8) + 8 * hf + v % 8;
-                    if (!sees(a, p, key0 + kk) || !(now_valid >> (kk / 8) & 1)) sc[sub][v] = -INFINITY;
+                for (int i = 0; i < QB; i++) {
+                    const int at = f * QB + i;
+                    if constexpr (NEXT) n.s[i][sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[f % AHEAD], qf[i][st], n.s[i][sub], 0, 0, 0);
+                    if constexpr (WEIGH) weights_upto(c, at * UNDER_SCORES / MM, (at + 1) * UNDER_SCORES / MM);
+                    SB;
                 }
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int sub = 0; sub < 2; sub++)
-#pragma unroll
-            for (int v = 0; v < 16; v++) mx = fmaxf(mx, sc[sub][v]);
-        mx = halves_max(mx) * a.scale_log2e;
-        if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0) {  // some row outgrew the maximum it uses by 2^8
-            const float mn = mx > m_run + 8.0f ? mx : m_run, alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - mn);
-            m_run = mn;
-            l_run *= alpha;
-#pragma unroll
-            for (int mt = 0; mt < MT; mt++)
-#pragma unroll
-                for (int v = 0; v < 16; v++) o[mt][v] *= alpha;
-        }
-        const float neg = m_run == -INFINITY ? 0.0f : -m_run;
-        bf16x8 pf[4];  // (weights rounded once, as the operand of the matrix instruction; the normaliser adds them unrounded)
-        float lsum = 0.0f;
-#pragma unroll
-        for (int sub = 0; sub < 2; sub++)
-#pragma unroll
-            for (int v = 0; v < 16; v++) {
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][v], a.scale_log2e, neg));
-                lsum += w;
-                pf[2 * sub + v / 8][v % 8] = (bf16)w;
             }
-        l_run += lsum;
+        }
+    };
+    float mx[QB];
+    // values of a tile, beside its last weights and the maxima of the scores in n
+    auto values = [&](auto next, unsigned sv, Scores &c, Scores &n) {
+        constexpr bool NEXT = decltype(next)::value;
+        constexpr int MM = 4 * MT * QB, LATE = PAIRS - UNDER_SCORES;
+#pragma unroll
+        for (int i = 0; i < QB; i++) mx[i] = -INFINITY;
+        bf16x8 vf[AHEAD];
+#pragma unroll
+        for (int g = 0; g < AHEAD - 1; g++) vf[g] = value_frag(sv, g / MT, g % MT);
 #pragma unroll
         for (int ks = 0; ks < 4; ks++)
 #pragma unroll
             for (int mt = 0; mt < MT; mt++) {
-                const int r = mt * 32 + frow;
-                const bf16x8 vf = sv[r * 8 + ((2 * ks + hf) ^ ((r >> 1) & 7))];
-                o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[ks], o[mt], 0, 0, 0);
+                const int g = ks * MT + mt;
+                if (g + AHEAD - 1 < 4 * MT) vf[(g + AHEAD - 1) % AHEAD] = value_frag(sv, (g + AHEAD - 1) / MT, (g + AHEAD - 1) % MT);
+#pragma unroll
+                for (int i = 0; i < QB; i++) {
+                    const int at = g * QB + i, half = MM / 2;
+                    o[i][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[g % AHEAD], pf[i][ks], o[i][mt], 0, 0, 0);
+                    if (at < half) {
+                        weights_upto(c, UNDER_SCORES + at * LATE / half, UNDER_SCORES + (at + 1) * LATE / half);
+                        if (at == half - 1) settle(c, PAIRS - 1);
+                    } else if constexpr (NEXT) {
+#pragma unroll
+                        for (int u = (at - half) * PAIRS / half; u < (at - half + 1) * PAIRS / half; u++) {
+                            const int r = u % QB, k = 2 * (u / QB);
+                            mx[r] = fmaxf(fmaxf(mx[r], n.s[r][k / 16][k % 16]), n.s[r][k / 16][k % 16 + 1]);
+                        }
+                    }
+                    SB;
+                }
             }
+    };
+    auto mask = [&](int key0, unsigned valid, Scores &n) {
+        if (valid != 0xFF || key0 + KT - 1 > p_lo || (a.window && p_hi - key0 >= a.window && key0 + KT > a.sinks)) {
+            int hf_ = hf;
+            asm volatile("" : "+v"(hf_));  // (nothing of this is kept in registers over the tiles that need none of it)
+            const unsigned ok = valid >> hf_;
+            const int k0 = key0 + 8 * hf_, sinks = a.window ? a.sinks - k0 : KT;
+#pragma unroll
+            for (int i = 0; i < QB; i++) {
+                const int last = p[i] - k0, from = a.window ? last - a.window + 1 : 0;  // of the lane's keys, counted from k0
+#pragma unroll
+                for (int sub = 0; sub < 2; sub++)
+#pragma unroll
+                    for (int v = 0; v < 16; v++) {
+                        const int kk = 32 * sub + 16 * (v / 8) + v % 8;
+                        const bool seen = (kk <= last) & ((kk >= from) | (kk < sinks)) & ((ok >> (kk / 8) & 1) != 0);
+                        n.s[i][sub][v] = seen ? n.s[i][sub][v] : -INFINITY;
+                    }
+            }
+        }
+    };
+    auto follow = [&]() {  // the maximum in use follows when some row outgrew it by 2^8: terms up to 256 harm nothing
+        bool outgrown = false;
+#pragma unroll
+        for (int i = 0; i < QB; i++) {
+            mx[i] = halves_max(mx[i]) * a.scale_log2e;
+            outgrown |= mx[i] > m_run[i] + 8.0f;
+        }
+        if (__builtin_amdgcn_ballot_w64(outgrown) != 0) {
+            // In place by hand: as plain products the sums get second registers and a copy on the common path, 64 of them at DH = 128.  The matrix
+            // instructions' results may be read after the pause (at most 19 wait states).
+            asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < QB; i++) {
+                const float mn = mx[i] > m_run[i] + 8.0f ? mx[i] : m_run[i], alpha = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - mn);
+                m_run[i] = mn;
+                l_run[i] *= alpha;
+#pragma unroll
+                for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+                    for (int v = 0; v < 16; v++) {
+                        float x = o[i][mt][v];
+                        asm volatile("v_mul_f32 %0, %0, %1" : "+v"(x) : "v"(alpha));
+                        o[i][mt][v] = x;
+                    }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < QB; i++) neg[i] = m_run[i] == -INFINITY ? 0.0f : -m_run[i];
+    };
+    // Group x of the loads: the values of tile x and the keys of tile x + 1, into slots x and x + 1 (modulo SLOTS).  Past the end the last tile is loaded again,
+    // into slots that nobody reads any more, so that the waits need no cases.
+    uint64_t valid = 0;  // byte i: valid chunks of tile x + i
+    const bool paged_tiles = a.page_shift >= 6;
+    int64_t start = 0;   // page_start of the tile whose keys were requested last
+    auto issue_k = [&](int x, int slot, int byte) {
+        want_pages(x);
+        if (paged_tiles) {
+            bool there;
+            start = page_start(x, there);
+            issue_k_at(start, (bl.at(x) * KT) & (page - 1), slot);
+            valid |= (uint64_t)(there ? 0xFF : 0) << (8 * byte);
+        } else {
+            issue_k_small(x, slot);
+            valid |= (uint64_t)valid_small(x) << (8 * byte);
+        }
+    };
+    auto issue = [&](int x, int slot, int byte) {
+        const int here = min(x, x1 - 1);
+        if (paged_tiles) issue_v_at(start, (bl.at(here) * KT) & (page - 1), slot);
+        else issue_v_small(here, slot);
+        issue_k(min(x + 1, x1 - 1), slot + 1 == SLOTS ? 0 : slot + 1, byte + 1);
+    };
+    auto meet = [&](auto left) {  // all but the newest `left` groups have landed, everybody's
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(left)::value * 2 * KI) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    if (x0 < x1) {
+        Scores s0, s1;
+        issue_k(x0, 0, 0);
+#pragma unroll
+        for (int g = 0; g < LEAD; g++) issue(x0 + g, g, g);
+        meet(std::integral_constant<int, LEAD>());
+        scores(yes, no, at_tile(k_lane, 0), s0, s1);
+        mask(bl.at(x0) * KT, (unsigned)valid & 0xFF, s0);
+#pragma unroll
+        for (int i = 0; i < QB; i++) {
+            mx[i] = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < 32; k++) mx[i] = fmaxf(mx[i], s0.s[i][k / 16][k % 16]);
+        }
+        follow();
+        int slot = 0;  // of tile x
+        auto after = [&](int n) { return slot + n >= SLOTS ? slot + n - SLOTS : slot + n; };
+        auto arrive = [&](int x) {  // tile x's values and tile x + 1's keys have landed
+            meet(std::integral_constant<int, LEAD - 1>());
+            issue(x + LEAD, after(LEAD), LEAD);
+            const int key0 = bl.at(x) * KT;
+            const unsigned here = (unsigned)valid & 0xFF;
+            if (here != 0xFF || key0 + KT - 1 > p_hi) {
+                // values no row of the workgroup may use: out of the product, where p = 0 would not keep an infinity or a NaN out
+                bf16x8 *sv = smem + (SLOTS + slot) * HALF;
+                int id = threadIdx.x;
+                asm volatile("" : "+v"(id));
+                for (; id < HALF; id += NW * 64) {
+                    const int r = id / 8, ch = (id % 8) ^ ((r >> 1) & 7);
+                    bf16x8 v = sv[id];
+#pragma unroll
+                    for (int e = 0; e < 8; e++)
+                        if (!(here >> ch & 1) || key0 + 8 * ch + e > p_hi) v[e] = (bf16)0.0f;
+                    sv[id] = v;
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            }
+        };
+        // tile x, whose scores are in c; the next tile's go to n
+        auto step = [&](int x, Scores &c, Scores &n) {
+            arrive(x);
+            scores(yes, yes, at_tile(k_lane, after(1)), n, c);
+            mask(bl.at(x + 1) * KT, (unsigned)(valid >> 8) & 0xFF, n);
+            values(yes, at_tile(v_lane, slot), c, n);
+            follow();
+            valid >>= 8;
+            slot = after(1);
+        };
+        auto last = [&](int x, Scores &c) {
+            arrive(x);
+            scores(no, yes, 0u, c, c);
+            values(no, at_tile(v_lane, slot), c, c);
+        };
+        int x = x0;
+        for (; x + 1 < x1; x++) {
+            step(x, s0, s1);
+            s0 = s1;
+        }
+        last(x, s0);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (loads in flight own their slots)
     }
-    const float l = halves_sum(l_run);
-    bool bad = !(l < INFINITY);
+#undef SB
+    const PagedArgs z = late_args();
+    bool bad = false;
 #pragma unroll
-    for (int mt = 0; mt < MT; mt++)
+    for (int i = 0; i < QB; i++) {
+        const float l = halves_sum(l_run[i]);
+        const int R = W0 + 32 * i + frow, tok = R / z.group, head = kvh * z.group + R - tok * z.group, row = s.start + tok;
+        if (R >= R1) continue;
+        bad |= !(l < INFINITY);
 #pragma unroll
-        for (int v = 0; v < 16; v++) bad |= !(fabsf(o[mt][v]) < INFINITY);
-    const int row = s.start + tok;
-    if (R < R1) {
-        if (a.nsplit > 1) {
-            float *part = part_row<DH>(a, row, head, split);
+        for (int mt = 0; mt < MT; mt++)
+#pragma unroll
+            for (int v = 0; v < 16; v++) bad |= !(fabsf(o[i][mt][v]) < INFINITY);
+        if (z.nsplit > 1) {
+            float *part = part_row<DH>(z, row, head, split);
 #pragma unroll
             for (int mt = 0; mt < MT; mt++)
 #pragma unroll
-                for (int v = 0; v < 16; v++) part[mt * 32 + 8 * (v / 4) + 4 * hf + v % 4] = o[mt][v];
+                for (int v = 0; v < 16; v++) part[mt * 32 + 8 * (v / 4) + 4 * hf + v % 4] = o[i][mt][v];
             if (hf == 0) {
-                part[DH] = m_run;
+                part[DH] = m_run[i];
                 part[DH + 1] = l;
             }
         } else {
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            bf16 *dst = out_row<bf16, DH>(a, row, head);
+            bf16 *dst = out_row<bf16, DH>(z, row, head);
 #pragma unroll
             for (int mt = 0; mt < MT; mt++)
 #pragma unroll
                 for (int g = 0; g < 4; g++) {
                     bf16x4 pk;
 #pragma unroll
-                    for (int j = 0; j < 4; j++) pk[j] = (bf16)(o[mt][4 * g + j] * inv);
+                    for (int j = 0; j < 4; j++) pk[j] = (bf16)(o[i][mt][4 * g + j] * inv);
                     *(bf16x4 *)(dst + mt * 32 + 8 * g + 4 * hf) = pk;
                 }
         }
     }
-    if (__builtin_amdgcn_ballot_w64(bad && R < R1) != 0)
-        for (int i = 0; i < 32 && R0 + wave * 32 + i < R1; i++) {
-            const int RR = R0 + wave * 32 + i, tk = RR / a.group;
-            plain_row<bf16, DH, KT>(a, s, bl, x0, x1, kvh, s.start + tk, kvh * a.group + RR - tk * a.group, base + tk, split);
+    if (__builtin_amdgcn_ballot_w64(bad) != 0)
+        for (int r = W0; r < W0 + 32 * QB && r < R1; r++) {
+            const int tk = r / z.group;
+            plain_row<bf16, DH, KT>(z, s, bl, x0, x1, kvh, s.start + tk, kvh * z.group + r - tk * z.group, base + tk, split);
         }
 }
 
@@ -713,7 +952,7 @@ int shift_of(int page) {
     return s;
 }
 
-constexpr int kFlashRows = 128;
+constexpr int kFlashRows = 256;
 
 // bound of the tiles of `rows` rows, of one key head
 int64_t tiles_of(int N, int B, int group, int rows) {
@@ -737,11 +976,23 @@ Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, 
     return p;
 }
 
+// More than 64 KB of LDS has to be asked for, once per kernel and device.
+int allow_lds(const void *kernel, int bytes) {
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess || device < 0) return GR4AD_EHIP;
+    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess ? GR4AD_OK : GR4AD_EHIP;
+}
+
 template <typename T, int DH> int launch_rows(const PagedArgs &a, bool flash, hipStream_t st) {
     const int64_t grid = (flash ? tiles_of(a.N, a.B, a.group, kFlashRows) : a.tiles) * a.Hkv * a.nsplit;
     if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
     if constexpr (sizeof(T) == 2 && DH >= 32) {
-        if (flash) hipLaunchKernelGGL((paged_flash<DH>), dim3((unsigned)grid), dim3(256), 64 * DH * 8, st, a);
+        if (flash) {
+            constexpr int NW = kFlashRows / 32, SLOTS = 4, LDS = 2 * SLOTS * 64 * DH * 2;
+            const int s = allow_lds((const void *)paged_flash<DH, NW, SLOTS>, LDS);
+            if (s) return s;
+            hipLaunchKernelGGL((paged_flash<DH, NW, SLOTS>), dim3((unsigned)grid), dim3(NW * 64), LDS, st, a);
+        }
     }
     if (!flash) hipLaunchKernelGGL((paged_rows<T, DH>), dim3((unsigned)grid), dim3(256), 0, st, a);
     GR4AD_LAUNCH_CHECK();
