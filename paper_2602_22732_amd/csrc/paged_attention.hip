@@ -240,12 +240,13 @@ template <int DH> struct Frags<bf16, DH> {
     }
     // key of the block behind row r of S^T's tile u
     __device__ __forceinline__ static int key_of(int u, int r) { return 8 * (r / 4) + 4 * u + r % 4; }
-    __device__ __forceinline__ void load_k(const bf16 *const (&half)[2], int page) {  // half: this head's keys of 16 of the block's keys
+    // k0: this head's keys from the block's first on, k1: from its key 16 on (v0, v1: their values)
+    __device__ __forceinline__ void load_k(const bf16 *k0, const bf16 *k1) {
         const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
+        const bf16 *base = r < 8 ? k0 : k1;  // (key_of(u, r) < 16)
 #pragma unroll
         for (int u = 0; u < 2; u++) {
-            const int key = key_of(u, r);
-            const bf16 *src = (key < 16 ? half[0] : half[1]) + (key % 16) * DH + 8 * c;
+            const bf16 *src = base + (key_of(u, r) % 16) * DH + 8 * c;
 #pragma unroll
             for (int f = 0; f < KF; f++) {
                 if (DH % 32 == 0 || 8 * c < DH) k[u][f] = *(const bf16x8 *)(src + 32 * f);
@@ -253,11 +254,12 @@ template <int DH> struct Frags<bf16, DH> {
             }
         }
     }
-    __device__ __forceinline__ void load_v(const bf16 *const (&half)[2], int page) {
+    __device__ __forceinline__ void load_v(const bf16 *v0, const bf16 *v1, int page) {
         const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
-        const bf16 *src = (c < 2 ? half[0] : half[1]) + (8 * c) % 16;
+        const bf16 *src = (c < 2 ? v0 : v1) + (8 * c) % 16 + r * page;
+        asm volatile("" : "+s"(page));  // (its multiples are formed here: kept over the loop they cost scalar registers that spill)
 #pragma unroll
-        for (int t = 0; t < VF; t++) v[t] = *(const bf16x8 *)(src + (16 * t + r) * page);
+        for (int t = 0; t < VF; t++) v[t] = *(const bf16x8 *)(src + 16 * t * page);
     }
     __device__ __forceinline__ void scores(floatx4 (&s)[2], const bf16x8 (&q)[KF]) const {
 #pragma unroll
@@ -305,15 +307,17 @@ template <int DH> struct Frags<float, DH> {
         }
     }
     __device__ __forceinline__ static int key_of(int, int r) { return r; }
-    __device__ __forceinline__ void load_k(const float *const (&half)[2], int page) {
+    __device__ __forceinline__ void load_k(const float *k0, const float *) {
         const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
 #pragma unroll
-        for (int f = 0; f < KF; f++) k[f] = *(const floatx4 *)(half[0] + r * DH + 16 * f + 4 * c);
+        for (int f = 0; f < KF; f++) k[f] = *(const floatx4 *)(k0 + r * DH + 16 * f + 4 * c);
     }
-    __device__ __forceinline__ void load_v(const float *const (&half)[2], int page) {
+    __device__ __forceinline__ void load_v(const float *v0, const float *, int page) {
         const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
+        const float *src = v0 + r * page + 4 * c;
+        asm volatile("" : "+s"(page));
 #pragma unroll
-        for (int t = 0; t < VF; t++) v[t] = *(const floatx4 *)(half[0] + (16 * t + r) * page + 4 * c);
+        for (int t = 0; t < VF; t++) v[t] = *(const floatx4 *)(src + 16 * t * page);
     }
     __device__ __forceinline__ void scores(floatx4 (&s)[1], const floatx4 (&q)[KF]) const {
         s[0] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -352,7 +356,7 @@ __device__ __forceinline__ float query_sum(float v) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
-template <typename T, int DH> __global__ __launch_bounds__(256) void paged_rows(PagedArgs a) {
+template <typename T, int DH> __global__ __launch_bounds__(256, DH == 128 ? 2 : 4) void paged_rows(PagedArgs a) {
     using F = Frags<T, DH>;
     constexpr int KB = F::KB, VF = F::VF, NW = 4;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, c = lane / 16;
@@ -379,24 +383,24 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void paged_rows(
         }
         return __builtin_amdgcn_readlane(ids, pg - ids_from);
     };
-    struct Source { const T *k[2], *v[2]; int valid; };  // valid: bit i: keys 16 i .. 16 i + 15 of the block lie on a page that exists
+    struct Source { const T *k0, *k1, *v0, *v1; int valid; };  // valid: bit i: keys 16 i .. 16 i + 15 of the block lie on a page that exists
     auto source = [&](int x) {
         Source r;
         const int key = bl.at(x) * KB, id = page_id(key), slot = key & (page - 1);
         const bool there = id >= 0 && id < a.n_pages;
         const int64_t hd = (int64_t)(there ? id : 0) * a.Hkv + kvh;
         r.valid = there ? 3 : 0;
-        r.k[0] = (const T *)a.k + (hd * page + slot) * DH;
-        r.v[0] = (const T *)a.v + hd * DH * page + slot;
-        r.k[1] = r.k[0] + 16 * DH;
-        r.v[1] = r.v[0] + 16;
+        r.k0 = (const T *)a.k + (hd * page + slot) * DH;
+        r.v0 = (const T *)a.v + hd * DH * page + slot;
+        r.k1 = r.k0 + 16 * DH;
+        r.v1 = r.v0 + 16;
         if (KB == 32 && page == 16) {  // the block's second half lies on the next page
             const int id1 = page_id(key + 16);
             const bool there1 = id1 >= 0 && id1 < a.n_pages;
             const int64_t hd1 = (int64_t)(there1 ? id1 : 0) * a.Hkv + kvh;
             r.valid = (there ? 1 : 0) | (there1 ? 2 : 0);
-            r.k[1] = (const T *)a.k + hd1 * page * DH;
-            r.v[1] = (const T *)a.v + hd1 * DH * page;
+            r.k1 = (const T *)a.k + hd1 * page * DH;
+            r.v1 = (const T *)a.v + hd1 * DH * page;
         }
         return r;
     };
@@ -406,19 +410,17 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void paged_rows(
 #pragma unroll
     for (int t = 0; t < VF; t++) o[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
     float m_run = -INFINITY, l_run = 0.0f;
-    Source src = {};
-    if (x0 < x1) {
-        src = source(x0);
-        f.load_k(src.k, page);
-        f.load_v(src.v, page);
-    }
-    for (int x = x0; x < x1; x++) {
+    // One block; NEXT: the keys and values of the next are requested when this one's have been used.  (No branch stands between a request and its use:
+    // the compiler would wait for everything behind it.)
+    Source src;
+    auto block = [&](auto next, int x) {
+        constexpr bool NEXT = decltype(next)::value;
         const int key0 = bl.at(x) * KB, valid = src.valid;
         floatx4 sc[F::TILES];
         f.scores(sc, q);
-        if (x + 1 < x1) {
+        if constexpr (NEXT) {
             src = source(x + 1);
-            f.load_k(src.k, page);
+            f.load_k(src.k0, src.k1);
         }
         const bool whole = valid == 3 && key0 + KB - 1 <= p_lo && (!a.window || p_hi - key0 < a.window || key0 + KB <= a.sinks);
         if (!whole) {
@@ -443,10 +445,15 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void paged_rows(
             const float alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - mn);
             m_run = mn;
             l_run *= alpha;
+            asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");  // (in place by hand, as in paged_flash; the matrix instructions' results may be read after the pause)
 #pragma unroll
             for (int t = 0; t < VF; t++)
 #pragma unroll
-                for (int v = 0; v < 4; v++) o[t][v] *= alpha;
+                for (int v = 0; v < 4; v++) {
+                    float y = o[t][v];
+                    asm volatile("v_mul_f32 %0, %0, %1" : "+v"(y) : "v"(alpha));
+                    o[t][v] = y;
+                }
         }
         const float neg = m_run == -INFINITY ? 0.0f : -m_run;
 #pragma unroll
@@ -457,7 +464,14 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void paged_rows(
                 l_run += sc[u][v];
             }
         f.add_values(o, sc);
-        if (x + 1 < x1) f.load_v(src.v, page);
+        if constexpr (NEXT) f.load_v(src.v0, src.v1, page);
+    };
+    if (x0 < x1) {
+        src = source(x0);
+        f.load_k(src.k0, src.k1);
+        f.load_v(src.v0, src.v1, page);
+        for (int x = x0; x + 1 < x1; x++) block(std::true_type(), x);
+        block(std::false_type(), x1 - 1);
     }
     l_run = query_sum(l_run);
 
