@@ -225,6 +225,8 @@ __device__ __forceinline__ int page_numbers(const PagedArgs &a, int b, int first
 // Fragments of one block of keys as the two products take them.  bf16: v_mfma_f32_16x16x32_bf16, 32 keys; float32: v_mfma_f32_16x16x4_f32, 16 keys.
 // A lane holds row lane % 16 of the first operand and c = lane / 16 says which part of the contraction; of S^T it gets query lane % 16 and four rows.
 // bf16: key rows enter in an order that makes the eight keys a lane then holds of P consecutive, as its piece of V^T has them.
+// New tokens among a block's keys, [first, end) of it: k, v are where its key 0 would lie among their rows
+template <typename T> struct NewRows { const T *k, *v; int64_t stride; int first, end; };
 template <typename T, int DH> struct Frags;
 template <int DH> struct Frags<bf16, DH> {
     static constexpr int KB = 32, KF = (DH + 31) / 32, VF = DH / 16;
@@ -283,6 +285,32 @@ template <int DH> struct Frags<bf16, DH> {
 #pragma unroll
         for (int t = 0; t < VF; t++) o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], rest, o[t], 0, 0, 0);
     }
+    __device__ __forceinline__ void take_new(const NewRows<bf16> &n, bf16 *k0, bf16 *k1, bf16 *v0, bf16 *v1, int valid, int page) {
+        const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            const int key = key_of(u, r);
+            if (key < n.first || key >= n.end || 8 * c >= DH) continue;
+            const bf16 *src = n.k + (int64_t)key * n.stride + 8 * c;
+            bf16 *dst = (r < 8 ? k0 : k1) + (key % 16) * DH + 8 * c;
+#pragma unroll
+            for (int f = 0; f < KF; f++) {
+                k[u][f] = *(const bf16x8 *)(src + 32 * f);
+                if (valid >> (key / 16) & 1) *(bf16x8 *)(dst + 32 * f) = k[u][f];
+            }
+        }
+        bf16 *dst = (c < 2 ? v0 : v1) + (8 * c) % 16 + r * page;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            const int key = 8 * c + e;
+            if (key < n.first || key >= n.end) continue;
+#pragma unroll
+            for (int t = 0; t < VF; t++) {
+                v[t][e] = n.v[(int64_t)key * n.stride + 16 * t + r];
+                if (valid >> (key / 16) & 1) dst[16 * t * page + e] = v[t][e];
+            }
+        }
+    }
     // values of keys nobody in the tile may use (slots behind the last token): out of the product
     __device__ __forceinline__ void drop_values(int from) {
         const int c = threadIdx.x % 64 / 16;
@@ -331,6 +359,26 @@ template <int DH> struct Frags<float, DH> {
         for (int e = 0; e < 4; e++)
 #pragma unroll
             for (int t = 0; t < VF; t++) o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][e], p[0][e], o[t], 0, 0, 0);
+    }
+    __device__ __forceinline__ void take_new(const NewRows<float> &n, float *k0, float *, float *v0, float *, int valid, int page) {
+        const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
+        if (r >= n.first && r < n.end) {
+#pragma unroll
+            for (int f = 0; f < KF; f++) {
+                k[f] = *(const floatx4 *)(n.k + (int64_t)r * n.stride + 16 * f + 4 * c);
+                if (valid) *(floatx4 *)(k0 + r * DH + 16 * f + 4 * c) = k[f];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const int key = 4 * c + e;
+            if (key < n.first || key >= n.end) continue;
+#pragma unroll
+            for (int t = 0; t < VF; t++) {
+                v[t][e] = n.v[(int64_t)key * n.stride + 16 * t + r];
+                if (valid) v0[(16 * t + r) * page + key] = v[t][e];
+            }
+        }
     }
     __device__ __forceinline__ void drop_values(int from) {
         const int c = threadIdx.x % 64 / 16;
@@ -413,9 +461,14 @@ template <typename T, int DH> __global__ __launch_bounds__(256, DH == 128 ? 2 : 
     // One block; NEXT: the keys and values of the next are requested when this one's have been used.  (No branch stands between a request and its use:
     // the compiler would wait for everything behind it.)
     Source src;
-    auto block = [&](auto next, int x) {
-        constexpr bool NEXT = decltype(next)::value;
+    auto block = [&](auto next, auto fresh, int x) {
+        constexpr bool NEXT = decltype(next)::value, NEW = decltype(fresh)::value;
         const int key0 = bl.at(x) * KB, valid = src.valid;
+        if constexpr (NEW) {
+            const int64_t row = (int64_t)(s.start + key0 - base) * a.kv_stride + kvh * DH;
+            const NewRows<T> n = {(const T *)a.k_new + row, (const T *)a.v_new + row, a.kv_stride, base - key0, s.len - key0};
+            f.take_new(n, (T *)src.k0, (T *)src.k1, (T *)src.v0, (T *)src.v1, valid, page);
+        }
         floatx4 sc[F::TILES];
         f.scores(sc, q);
         if constexpr (NEXT) {
@@ -470,8 +523,20 @@ template <typename T, int DH> __global__ __launch_bounds__(256, DH == 128 ? 2 : 
         src = source(x0);
         f.load_k(src.k0, src.k1);
         f.load_v(src.v0, src.v1, page);
-        for (int x = x0; x + 1 < x1; x++) block(std::true_type(), x);
-        block(std::false_type(), x1 - 1);
+        constexpr std::true_type yes;
+        constexpr std::false_type no;
+        // From block xn on there are new tokens: they are read where they are and written into their pages by whoever walks their block.  (Several tiles of
+        // one sequence then write the same; the tile of a token's own row always walks it.)
+        int xn = x1;
+        if (a.k_new) {
+            const int first = max(base, 0) / KB;
+            xn = min(max(first < bl.first ? first : max(bl.first, first - bl.from + bl.first), x0), x1);
+        }
+        int x = x0;
+        for (; x < xn && x + 1 < x1; x++) block(yes, no, x);
+        for (; x + 1 < x1; x++) block(yes, yes, x);
+        if (x < xn) block(no, no, x);
+        else block(no, yes, x);
     }
     l_run = query_sum(l_run);
 
@@ -931,29 +996,44 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
         }
 }
 
-// Joins the workgroups' shares of a row: one wavefront per row.
-template <typename T, int DH> __global__ __launch_bounds__(256) void paged_join(PagedArgs a) {
-    const int lane = threadIdx.x % 64;
-    const int64_t w = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;  // (tile, key head, row)
+// Joins the workgroups' shares of a row: WAVES wavefronts per row, each with shares of its own.
+template <typename T, int DH, int WAVES> __global__ __launch_bounds__(256) void paged_join(PagedArgs a) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, part_of = wave % WAVES;
+    const int64_t w = (int64_t)blockIdx.x * (4 / WAVES) + wave / WAVES;  // (tile, key head, row)
     const int r = (int)(w % kRows), kvh = (int)(w / kRows % a.Hkv);
     Sequence s;
-    if (!find_sequence(a, w / (kRows * a.Hkv), [&](int m, int) { return (m * a.group + kRows - 1) / kRows; }, s)) return;
-    const int R = s.tile * kRows + r;
-    if (R >= s.m * a.group) return;
+    const bool found = find_sequence(a, w / (kRows * a.Hkv), [&](int m, int) { return (m * a.group + kRows - 1) / kRows; }, s);
+    const int R = found ? s.tile * kRows + r : 0;
+    if (!found || R >= s.m * a.group) return;  // (all wavefronts of a row alike)
     const int tok = R / a.group, row = s.start + tok, head = kvh * a.group + R - tok * a.group;
     constexpr int E = (DH + 63) / 64;
     const float *part = part_row<DH>(a, row, head, 0);
-    float m = -INFINITY;
-    for (int i = lane; i < a.nsplit; i += 64) m = fmaxf(m, part[(int64_t)i * (DH + 2) + DH]);
-    m = wave_max(m);
-    float l = 0.0f, o[E] = {};
-    for (int i = 0; i < a.nsplit; i++) {
-        const float *x = part + (int64_t)i * (DH + 2);
-        const float mi = x[DH], f = mi == m ? 1.0f : __builtin_amdgcn_exp2f(mi - m);
-        l = fmaf(x[DH + 1], f, l);
+    float m = -INFINITY, l = 0.0f;  // of share `lane` (at most 64)
+    if (lane < a.nsplit) {
+        m = part[(int64_t)lane * (DH + 2) + DH];
+        l = part[(int64_t)lane * (DH + 2) + DH + 1];
+    }
+    const float most = wave_max(m), f = m == most ? (lane < a.nsplit ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m - most);
+    l = wave_sum(l * f);
+    float o[E] = {};
+    const int each = (a.nsplit + WAVES - 1) / WAVES, i1 = min((part_of + 1) * each, a.nsplit);
+#pragma unroll 8
+    for (int i = part_of * each; i < i1; i++) {
+        const float fi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), i));
 #pragma unroll
         for (int e = 0; e < E; e++)
-            if (lane + 64 * e < DH) o[e] = fmaf(x[lane + 64 * e], f, o[e]);
+            if (lane + 64 * e < DH) o[e] = fmaf(part[(int64_t)i * (DH + 2) + lane + 64 * e], fi, o[e]);
+    }
+    if (WAVES > 1) {
+        __shared__ float sums[4][64 * E];
+#pragma unroll
+        for (int e = 0; e < E; e++) sums[wave][lane + 64 * e] = o[e];
+        __syncthreads();
+        if (part_of) return;
+#pragma unroll
+        for (int x = 1; x < WAVES; x++)
+#pragma unroll
+            for (int e = 0; e < E; e++) o[e] += sums[x][lane + 64 * e];
     }
 #pragma unroll
     for (int e = 0; e < E; e++)
@@ -999,7 +1079,7 @@ int allow_lds(const void *kernel, int bytes) {
 
 template <typename T, int DH> int launch_rows(const PagedArgs &a, bool flash, hipStream_t st) {
     const int64_t grid = (flash ? tiles_of(a.N, a.B, a.group, kFlashRows) : a.tiles) * a.Hkv * a.nsplit;
-    if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
+    if (grid > 0x7fffffffLL || a.tiles * a.Hkv * kRows > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
     if constexpr (sizeof(T) == 2 && DH >= 32) {
         if (flash) {
             constexpr int NW = kFlashRows / 32, SLOTS = 4, LDS = 2 * SLOTS * 64 * DH * 2;
@@ -1011,7 +1091,9 @@ template <typename T, int DH> int launch_rows(const PagedArgs &a, bool flash, hi
     if (!flash) hipLaunchKernelGGL((paged_rows<T, DH>), dim3((unsigned)grid), dim3(256), 0, st, a);
     GR4AD_LAUNCH_CHECK();
     if (a.nsplit > 1) {
-        hipLaunchKernelGGL((paged_join<T, DH>), dim3((unsigned)(a.tiles * a.Hkv * kRows / 4)), dim3(256), 0, st, a);
+        const int64_t rows = a.tiles * a.Hkv * kRows;
+        if (a.nsplit >= 16) hipLaunchKernelGGL((paged_join<T, DH, 4>), dim3((unsigned)rows), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((paged_join<T, DH, 1>), dim3((unsigned)(rows / 4)), dim3(256), 0, st, a);
         GR4AD_LAUNCH_CHECK();
     }
     return GR4AD_OK;
@@ -1072,7 +1154,7 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
     PagedArgs a = {q, q_stride, k_new, v_new, kv_stride, q_start, seq_len, c.page_table, c.k_pages, c.v_pages, c.n_pages, shift_of(c.page_size), c.max_pages, B, N, H, c.H_kv,
                    H / c.H_kv, scale * 1.4426950408889634f, window > kMostKeys ? kMostKeys : window, sinks > kMostKeys ? kMostKeys : sinks, out, (float *)workspace, p.nsplit, p.tiles};
     const int e = dtype == GR4AD_BF16 ? 2 : 4;
-    if (k_new) {
+    if (k_new && p.flash) {  // (tiles of 16 rows take the new tokens where they are)
         int64_t tiles = (int64_t)N / kAppendKeys + 2 * (int64_t)B;
         if (tiles > N) tiles = N;
         const int64_t grid = tiles * c.H_kv;
