@@ -18,7 +18,7 @@
 
 namespace {
 
-constexpr int kRows = 16;       // rows of a tile
+constexpr int kRows = 16;       // rows of a tile of the join
 constexpr int kAppendKeys = 64; // positions of a tile of the update
 
 struct PagedArgs {
@@ -35,7 +35,6 @@ struct PagedArgs {
     void *out;
     float *part;        // [N][H][nsplit][DH + 2]: sums, maximum, normaliser (nsplit > 1)
     int nsplit;
-    int64_t tiles;      // bound of the tiles of 16 rows
 };
 
 struct Sequence { int b, tile, start, m, len; };  // tile: number inside the sequence
@@ -232,12 +231,12 @@ template <int DH> struct Frags<bf16, DH> {
     static constexpr int KB = 32, KF = (DH + 31) / 32, VF = DH / 16;
     bf16x8 k[2][KF], v[VF];
     __device__ __forceinline__ static bf16x8 zero() { return bf16x8{}; }
-    __device__ __forceinline__ static void load_q(bf16x8 (&q)[KF], const bf16 *row, bool valid) {
+    __device__ __forceinline__ static void load_q(bf16x8 (&q)[KF], const bf16 *row) {
         const int c = threadIdx.x % 64 / 16;
 #pragma unroll
         for (int f = 0; f < KF; f++) {
             q[f] = zero();
-            if (valid && 32 * f + 8 * c < DH) q[f] = *(const bf16x8 *)(row + 32 * f + 8 * c);
+            if (32 * f + 8 * c < DH) q[f] = *(const bf16x8 *)(row + 32 * f + 8 * c);
         }
     }
     // key of the block behind row r of S^T's tile u
@@ -311,14 +310,14 @@ template <int DH> struct Frags<bf16, DH> {
             }
         }
     }
-    // values of keys nobody in the tile may use (slots behind the last token): out of the product
-    __device__ __forceinline__ void drop_values(int from) {
+    // values of keys nobody in the tile may use (slots behind the last token, pages that do not exist): out of the product
+    __device__ __forceinline__ void drop_values(int from, int valid) {
         const int c = threadIdx.x % 64 / 16;
 #pragma unroll
         for (int t = 0; t < VF; t++)
 #pragma unroll
             for (int e = 0; e < 8; e++)
-                if (8 * c + e >= from) v[t][e] = (bf16)0.0f;
+                if (8 * c + e >= from || !(valid >> (c / 2) & 1)) v[t][e] = (bf16)0.0f;
     }
     static constexpr int TILES = 2;
     using Q = bf16x8[KF];
@@ -326,13 +325,10 @@ template <int DH> struct Frags<bf16, DH> {
 template <int DH> struct Frags<float, DH> {
     static constexpr int KB = 16, KF = DH / 16, VF = DH / 16;
     floatx4 k[KF], v[VF];
-    __device__ __forceinline__ static void load_q(floatx4 (&q)[KF], const float *row, bool valid) {
+    __device__ __forceinline__ static void load_q(floatx4 (&q)[KF], const float *row) {
         const int c = threadIdx.x % 64 / 16;
 #pragma unroll
-        for (int f = 0; f < KF; f++) {
-            q[f] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-            if (valid) q[f] = *(const floatx4 *)(row + 16 * f + 4 * c);
-        }
+        for (int f = 0; f < KF; f++) q[f] = *(const floatx4 *)(row + 16 * f + 4 * c);
     }
     __device__ __forceinline__ static int key_of(int, int r) { return r; }
     __device__ __forceinline__ void load_k(const float *k0, const float *) {
@@ -380,13 +376,13 @@ template <int DH> struct Frags<float, DH> {
             }
         }
     }
-    __device__ __forceinline__ void drop_values(int from) {
+    __device__ __forceinline__ void drop_values(int from, int valid) {
         const int c = threadIdx.x % 64 / 16;
 #pragma unroll
         for (int t = 0; t < VF; t++)
 #pragma unroll
             for (int e = 0; e < 4; e++)
-                if (4 * c + e >= from) v[t][e] = 0.0f;
+                if (4 * c + e >= from || !valid) v[t][e] = 0.0f;
     }
     static constexpr int TILES = 1;
     using Q = floatx4[KF];
@@ -404,22 +400,29 @@ __device__ __forceinline__ float query_sum(float v) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
-template <typename T, int DH> __global__ __launch_bounds__(256, DH == 128 ? 2 : 4) void paged_rows(PagedArgs a) {
+// MR groups of 16 rows per workgroup (each key read serves them all).
+template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH <= 64 ? 4 : 2) void paged_rows(PagedArgs a) {
     using F = Frags<T, DH>;
-    constexpr int KB = F::KB, VF = F::VF, NW = 4;
+    constexpr int KB = F::KB, VF = F::VF, NW = 4, ROWS = 16 * MR;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, c = lane / 16;
     const int split = blockIdx.x % a.nsplit, kvh = blockIdx.x / a.nsplit % a.Hkv, page = 1 << a.page_shift;
     Sequence s;
-    if (!find_sequence(a, blockIdx.x / (a.nsplit * a.Hkv), [&](int m, int) { return (m * a.group + kRows - 1) / kRows; }, s)) return;
-    const int R0 = s.tile * kRows, R1 = min(R0 + kRows, s.m * a.group), base = s.len - s.m;
+    if (!find_longest_first(a, blockIdx.x / (a.nsplit * a.Hkv), [&](int m, int) { return (m * a.group + ROWS - 1) / ROWS; }, s)) return;
+    const int R0 = s.tile * ROWS, R1 = min(R0 + ROWS, s.m * a.group), base = s.len - s.m;
     const int p_lo = base + R0 / a.group, p_hi = base + (R1 - 1) / a.group;
     const Blocks bl = visible_blocks<KB>(a, p_lo, p_hi);
     const int each = (bl.count + a.nsplit * NW - 1) / (a.nsplit * NW);
     const int x0 = min((split * NW + wave) * each, bl.count), x1 = min(x0 + each, bl.count);
 
-    const int R = R0 + n, tok = R / a.group, head = kvh * a.group + R - tok * a.group, p = R < R1 ? base + tok : -1;
-    typename F::Q q;
-    F::load_q(q, (const T *)a.q + (int64_t)(s.start + tok) * a.q_stride + head * DH, R < R1);
+    int p[MR];
+    typename F::Q q[MR];
+#pragma unroll
+    for (int i = 0; i < MR; i++) {
+        const int R = R0 + 16 * i + n, tok = R / a.group, head = kvh * a.group + R - tok * a.group;
+        p[i] = R < R1 ? base + tok : -1;
+        // (rows past the last repeat a token's: they are computed and dropped)
+        F::load_q(q[i], (const T *)a.q + (int64_t)(s.start + min(tok, s.m - 1)) * a.q_stride + head * DH);
+    }
 
     // page numbers: one of 64 successive pages per lane
     int ids = 0, ids_from = -64;
@@ -454,23 +457,29 @@ template <typename T, int DH> __global__ __launch_bounds__(256, DH == 128 ? 2 : 
     };
 
     F f;
-    floatx4 o[VF];
+    floatx4 o[MR][VF];
+    float m_run[MR], l_run[MR];
 #pragma unroll
-    for (int t = 0; t < VF; t++) o[t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    float m_run = -INFINITY, l_run = 0.0f;
-    // One block; NEXT: the keys and values of the next are requested when this one's have been used.  (No branch stands between a request and its use:
-    // the compiler would wait for everything behind it.)
+    for (int i = 0; i < MR; i++) {
+        m_run[i] = -INFINITY;
+        l_run[i] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < VF; t++) o[i][t] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    // One block; NEXT: the keys and values of the next are requested when this one's have been used; NEW: there may be new tokens in it.  (No branch stands
+    // between a request and its use: the compiler would wait for everything behind it.)
     Source src;
     auto block = [&](auto next, auto fresh, int x) {
         constexpr bool NEXT = decltype(next)::value, NEW = decltype(fresh)::value;
         const int key0 = bl.at(x) * KB, valid = src.valid;
         if constexpr (NEW) {
             const int64_t row = (int64_t)(s.start + key0 - base) * a.kv_stride + kvh * DH;
-            const NewRows<T> n = {(const T *)a.k_new + row, (const T *)a.v_new + row, a.kv_stride, base - key0, s.len - key0};
-            f.take_new(n, (T *)src.k0, (T *)src.k1, (T *)src.v0, (T *)src.v1, valid, page);
+            const NewRows<T> nr = {(const T *)a.k_new + row, (const T *)a.v_new + row, a.kv_stride, base - key0, s.len - key0};
+            f.take_new(nr, (T *)src.k0, (T *)src.k1, (T *)src.v0, (T *)src.v1, valid, page);
         }
-        floatx4 sc[F::TILES];
-        f.scores(sc, q);
+        floatx4 sc[MR][F::TILES];
+#pragma unroll
+        for (int i = 0; i < MR; i++) f.scores(sc[i], q[i]);
         if constexpr (NEXT) {
             src = source(x + 1);
             f.load_k(src.k0, src.k1);
@@ -478,45 +487,59 @@ template <typename T, int DH> __global__ __launch_bounds__(256, DH == 128 ? 2 : 
         const bool whole = valid == 3 && key0 + KB - 1 <= p_lo && (!a.window || p_hi - key0 < a.window || key0 + KB <= a.sinks);
         if (!whole) {
 #pragma unroll
+            for (int i = 0; i < MR; i++)
+#pragma unroll
+                for (int u = 0; u < F::TILES; u++)
+#pragma unroll
+                    for (int v = 0; v < 4; v++) {
+                        const int kk = F::key_of(u, 4 * c + v);
+                        if (!sees(a, p[i], key0 + kk) || !(valid >> (kk / 16) & 1)) sc[i][u][v] = -INFINITY;
+                    }
+            if (key0 + KB - 1 > p_hi || valid != 3) f.drop_values(p_hi + 1 - key0, valid);
+        }
+        float mx[MR];
+        bool outgrown = false;
+#pragma unroll
+        for (int i = 0; i < MR; i++) {
+            mx[i] = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < F::TILES; u++)
+#pragma unroll
+                for (int v = 0; v < 4; v++) mx[i] = fmaxf(mx[i], sc[i][u][v]);
+            mx[i] = query_max(mx[i]) * a.scale_log2e;
+            outgrown |= mx[i] > m_run[i] + 8.0f;
+        }
+        // the maximum in use follows when it is outgrown by 2^8: terms up to 256 harm nothing
+        if (__builtin_amdgcn_ballot_w64(outgrown) != 0) {
+            asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");  // (in place by hand, as in paged_flash; the matrix instructions' results may be read after the pause)
+#pragma unroll
+            for (int i = 0; i < MR; i++) {
+                const float mn = mx[i] > m_run[i] + 8.0f ? mx[i] : m_run[i];
+                const float alpha = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - mn);
+                m_run[i] = mn;
+                l_run[i] *= alpha;
+#pragma unroll
+                for (int t = 0; t < VF; t++)
+#pragma unroll
+                    for (int v = 0; v < 4; v++) {
+                        float y = o[i][t][v];
+                        asm volatile("v_mul_f32 %0, %0, %1" : "+v"(y) : "v"(alpha));
+                        o[i][t][v] = y;
+                    }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MR; i++) {
+            const float neg = m_run[i] == -INFINITY ? 0.0f : -m_run[i];
+#pragma unroll
             for (int u = 0; u < F::TILES; u++)
 #pragma unroll
                 for (int v = 0; v < 4; v++) {
-                    const int kk = F::key_of(u, 4 * c + v);
-                    if (!sees(a, p, key0 + kk) || !(valid >> (kk / 16) & 1)) sc[u][v] = -INFINITY;
+                    sc[i][u][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[i][u][v], a.scale_log2e, neg));
+                    l_run[i] += sc[i][u][v];
                 }
-            if (key0 + KB - 1 > p_hi) f.drop_values(p_hi + 1 - key0);
+            f.add_values(o[i], sc[i]);
         }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < F::TILES; u++)
-#pragma unroll
-            for (int v = 0; v < 4; v++) mx = fmaxf(mx, sc[u][v]);
-        mx = query_max(mx) * a.scale_log2e;
-        // the maximum in use follows when it is outgrown by 2^8: terms up to 256 harm nothing
-        if (__builtin_amdgcn_ballot_w64(mx > m_run + 8.0f) != 0) {
-            const float mn = mx > m_run + 8.0f ? mx : m_run;
-            const float alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - mn);
-            m_run = mn;
-            l_run *= alpha;
-            asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");  // (in place by hand, as in paged_flash; the matrix instructions' results may be read after the pause)
-#pragma unroll
-            for (int t = 0; t < VF; t++)
-#pragma unroll
-                for (int v = 0; v < 4; v++) {
-                    float y = o[t][v];
-                    asm volatile("v_mul_f32 %0, %0, %1" : "+v"(y) : "v"(alpha));
-                    o[t][v] = y;
-                }
-        }
-        const float neg = m_run == -INFINITY ? 0.0f : -m_run;
-#pragma unroll
-        for (int u = 0; u < F::TILES; u++)
-#pragma unroll
-            for (int v = 0; v < 4; v++) {
-                sc[u][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[u][v], a.scale_log2e, neg));
-                l_run += sc[u][v];
-            }
-        f.add_values(o, sc);
         if constexpr (NEXT) f.load_v(src.v0, src.v1, page);
     };
     if (x0 < x1) {
@@ -538,44 +561,48 @@ template <typename T, int DH> __global__ __launch_bounds__(256, DH == 128 ? 2 : 
         if (x < xn) block(no, no, x);
         else block(no, yes, x);
     }
-    l_run = query_sum(l_run);
 
-    // the wavefronts' stretches, joined in their order
+    // the wavefronts' stretches, joined in their order, 16 rows at a time
     const PagedArgs z = late_args();
-    __shared__ float sm[NW][kRows], sl[NW][kRows];
-    __shared__ __attribute__((aligned(16))) float so[NW][kRows][DH + 4];
-    if (c == 0) {
-        sm[wave][n] = m_run;
-        sl[wave][n] = l_run;
-    }
-#pragma unroll
-    for (int t = 0; t < VF; t++) *(floatx4 *)&so[wave][n][16 * t + 4 * c] = o[t];
-    __syncthreads();
+    __shared__ float sm[NW][16], sl[NW][16];
+    __shared__ __attribute__((aligned(16))) float so[NW][16][DH + 4];
     bool bad = false;
-    for (int i = threadIdx.x; i < kRows * DH; i += 256) {
-        const int r = i / DH, d = i % DH, RR = R0 + r;
-        if (RR >= R1) continue;
-        float m = sm[0][r];
 #pragma unroll
-        for (int w = 1; w < NW; w++) m = fmaxf(m, sm[w][r]);
-        float l = 0.0f, v = 0.0f;
-#pragma unroll
-        for (int w = 0; w < NW; w++) {
-            const float f_ = sm[w][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][r] - m);
-            l = fmaf(sl[w][r], f_, l);
-            v = fmaf(so[w][r][d], f_, v);
-            bad |= !(fabsf(so[w][r][d]) < INFINITY) || !(sl[w][r] < INFINITY);
+    for (int i = 0; i < MR; i++) {
+        const float l = query_sum(l_run[i]);
+        if (i) __syncthreads();
+        if (c == 0) {
+            sm[wave][n] = m_run[i];
+            sl[wave][n] = l;
         }
-        const int tk = RR / z.group, row = s.start + tk, hd = kvh * z.group + RR - tk * z.group;
-        if (z.nsplit > 1) {
-            float *part = part_row<DH>(z, row, hd, split);
-            part[d] = v;
-            if (d == 0) {
-                part[DH] = m;
-                part[DH + 1] = l;
+#pragma unroll
+        for (int t = 0; t < VF; t++) *(floatx4 *)&so[wave][n][16 * t + 4 * c] = o[i][t];
+        __syncthreads();
+        for (int j = threadIdx.x; j < 16 * DH; j += 256) {
+            const int r = j / DH, d = j % DH, RR = R0 + 16 * i + r;
+            if (RR >= R1) continue;
+            float m = sm[0][r];
+#pragma unroll
+            for (int w = 1; w < NW; w++) m = fmaxf(m, sm[w][r]);
+            float sum = 0.0f, v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; w++) {
+                const float f_ = sm[w][r] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][r] - m);
+                sum = fmaf(sl[w][r], f_, sum);
+                v = fmaf(so[w][r][d], f_, v);
+                bad |= !(fabsf(so[w][r][d]) < INFINITY) || !(sl[w][r] < INFINITY);
             }
-        } else {
-            out_row<T, DH>(z, row, hd)[d] = from_f<T>(l == 0.0f ? 0.0f : v / l);
+            const int tk = RR / z.group, row = s.start + tk, hd = kvh * z.group + RR - tk * z.group;
+            if (z.nsplit > 1) {
+                float *part = part_row<DH>(z, row, hd, split);
+                part[d] = v;
+                if (d == 0) {
+                    part[DH] = m;
+                    part[DH + 1] = sum;
+                }
+            } else {
+                out_row<T, DH>(z, row, hd)[d] = from_f<T>(sum == 0.0f ? 0.0f : v / sum);
+            }
         }
     }
     if (__syncthreads_or(bad)) {
@@ -1054,14 +1081,17 @@ int64_t tiles_of(int N, int B, int group, int rows) {
     return n < all ? n : all;
 }
 
-// flash: tiles of 128 rows share the staged keys; otherwise 16 rows.  nsplit: workgroups that share a tile's keys.
-struct Plan { bool flash; int64_t tiles; int nsplit; size_t bytes; };
+// rows: of a tile: 16 or 32 (paged_rows), or 256 that share staged keys (paged_flash).  nsplit: workgroups that share a tile's keys.
+struct Plan { int rows; int64_t tiles, join_tiles; int nsplit; size_t bytes; };
 Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, int max_pages, int window, int sinks) {
     Plan p;
     const int group = H / Hkv;
-    p.flash = dtype == GR4AD_BF16 && dh >= 32 && (int64_t)N * group >= 64 * (int64_t)B;
-    p.tiles = tiles_of(N, B, group, kRows);
-    const int64_t blocks = (p.flash ? tiles_of(N, B, group, kFlashRows) : p.tiles) * Hkv, enough = p.flash ? 512 : 2048, least = p.flash ? 1024 : 256;
+    const int64_t rows = (int64_t)N * group / B;  // of a sequence and key head, on average
+    p.rows = rows <= 16 ? 16 : dtype == GR4AD_BF16 && dh >= 32 && rows >= 64 ? kFlashRows : 32;
+    p.tiles = tiles_of(N, B, group, p.rows);
+    p.join_tiles = tiles_of(N, B, group, kRows);
+    const bool flash = p.rows == kFlashRows;
+    const int64_t blocks = p.tiles * Hkv, enough = flash ? 256 : 2048, least = flash ? 1024 : 256;
     int64_t keys = (int64_t)max_pages * page;
     if (window && (int64_t)window + sinks + 64 < keys) keys = (int64_t)window + sinks + 64;
     const int64_t want = (enough + blocks - 1) / blocks, most = (keys + least - 1) / least, n = want < most ? want : most;
@@ -1077,33 +1107,33 @@ int allow_lds(const void *kernel, int bytes) {
     return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess ? GR4AD_OK : GR4AD_EHIP;
 }
 
-template <typename T, int DH> int launch_rows(const PagedArgs &a, bool flash, hipStream_t st) {
-    const int64_t grid = (flash ? tiles_of(a.N, a.B, a.group, kFlashRows) : a.tiles) * a.Hkv * a.nsplit;
-    if (grid > 0x7fffffffLL || a.tiles * a.Hkv * kRows > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
-    if constexpr (sizeof(T) == 2 && DH >= 32) {
-        if (flash) {
-            constexpr int NW = kFlashRows / 32, SLOTS = 4, LDS = 2 * SLOTS * 64 * DH * 2;
-            const int s = allow_lds((const void *)paged_flash<DH, NW, SLOTS>, LDS);
-            if (s) return s;
-            hipLaunchKernelGGL((paged_flash<DH, NW, SLOTS>), dim3((unsigned)grid), dim3(NW * 64), LDS, st, a);
-        }
+template <typename T, int DH> int launch_rows(const PagedArgs &a, const Plan &p, hipStream_t st) {
+    const int64_t grid = p.tiles * a.Hkv * a.nsplit, joined = p.join_tiles * a.Hkv * kRows;
+    if (grid > 0x7fffffffLL || joined > 0x7fffffffLL) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: %d rows of %d heads", a.N, a.H);
+    if (p.rows == 16) {
+        hipLaunchKernelGGL((paged_rows<T, DH, 1>), dim3((unsigned)grid), dim3(256), 0, st, a);
+    } else if (p.rows == 32) {
+        hipLaunchKernelGGL((paged_rows<T, DH, 2>), dim3((unsigned)grid), dim3(256), 0, st, a);
+    } else if constexpr (sizeof(T) == 2 && DH >= 32) {
+        constexpr int NW = kFlashRows / 32, SLOTS = 4, LDS = 2 * SLOTS * 64 * DH * 2;
+        const int s = allow_lds((const void *)paged_flash<DH, NW, SLOTS>, LDS);
+        if (s) return s;
+        hipLaunchKernelGGL((paged_flash<DH, NW, SLOTS>), dim3((unsigned)grid), dim3(NW * 64), LDS, st, a);
     }
-    if (!flash) hipLaunchKernelGGL((paged_rows<T, DH>), dim3((unsigned)grid), dim3(256), 0, st, a);
     GR4AD_LAUNCH_CHECK();
     if (a.nsplit > 1) {
-        const int64_t rows = a.tiles * a.Hkv * kRows;
-        if (a.nsplit >= 16) hipLaunchKernelGGL((paged_join<T, DH, 4>), dim3((unsigned)rows), dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((paged_join<T, DH, 1>), dim3((unsigned)(rows / 4)), dim3(256), 0, st, a);
+        if (a.nsplit >= 16) hipLaunchKernelGGL((paged_join<T, DH, 4>), dim3((unsigned)joined), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((paged_join<T, DH, 1>), dim3((unsigned)(joined / 4)), dim3(256), 0, st, a);
         GR4AD_LAUNCH_CHECK();
     }
     return GR4AD_OK;
 }
-template <typename T> int launch_width(const PagedArgs &a, int dh, bool flash, hipStream_t st) {
+template <typename T> int launch_width(const PagedArgs &a, int dh, const Plan &p, hipStream_t st) {
     switch (dh) {
-        case 16: return launch_rows<T, 16>(a, flash, st);
-        case 32: return launch_rows<T, 32>(a, flash, st);
-        case 64: return launch_rows<T, 64>(a, flash, st);
-        default: return launch_rows<T, 128>(a, flash, st);
+        case 16: return launch_rows<T, 16>(a, p, st);
+        case 32: return launch_rows<T, 32>(a, p, st);
+        case 64: return launch_rows<T, 64>(a, p, st);
+        default: return launch_rows<T, 128>(a, p, st);
     }
 }
 
@@ -1152,9 +1182,9 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
         return gr4ad_set_thread_error(GR4AD_EWORKSPACE, "paged attention: workspace of %zu bytes needed, 16-byte aligned", p.bytes);
     hipStream_t st = (hipStream_t)hip_stream;
     PagedArgs a = {q, q_stride, k_new, v_new, kv_stride, q_start, seq_len, c.page_table, c.k_pages, c.v_pages, c.n_pages, shift_of(c.page_size), c.max_pages, B, N, H, c.H_kv,
-                   H / c.H_kv, scale * 1.4426950408889634f, window > kMostKeys ? kMostKeys : window, sinks > kMostKeys ? kMostKeys : sinks, out, (float *)workspace, p.nsplit, p.tiles};
+                   H / c.H_kv, scale * 1.4426950408889634f, window > kMostKeys ? kMostKeys : window, sinks > kMostKeys ? kMostKeys : sinks, out, (float *)workspace, p.nsplit};
     const int e = dtype == GR4AD_BF16 ? 2 : 4;
-    if (k_new && p.flash) {  // (tiles of 16 rows take the new tokens where they are)
+    if (k_new && p.rows == kFlashRows) {  // (the smaller tiles take the new tokens where they are)
         int64_t tiles = (int64_t)N / kAppendKeys + 2 * (int64_t)B;
         if (tiles > N) tiles = N;
         const int64_t grid = tiles * c.H_kv;
@@ -1167,7 +1197,7 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
     // lengths lie on the device: counted on all pages of every sequence, an upper bound
     const double keys = (double)c.max_pages * c.page_size;
     ProfScope ps(KC_PAGED_ATTN, st, 4.0 * N * keys * H * c.dh, e * (2.0 * B * keys * c.H_kv * c.dh + 2.0 * N * H * c.dh));
-    return dtype == GR4AD_BF16 ? launch_width<bf16>(a, c.dh, p.flash, st) : launch_width<float>(a, c.dh, false, st);
+    return dtype == GR4AD_BF16 ? launch_width<bf16>(a, c.dh, p, st) : launch_width<float>(a, c.dh, p, st);
 }
 
 }  // extern "C"
