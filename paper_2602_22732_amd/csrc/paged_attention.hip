@@ -169,15 +169,19 @@ __device__ void plain_row(const PagedArgs &a, const Sequence &s, const Blocks &b
             if (!sees(a, p, key) || key >= s.len) continue;
             const int id = page_of(a, s.b, key), slot = key & (page - 1);
             if (id < 0 || id >= a.n_pages) continue;
-            const int64_t hd = (int64_t)id * a.Hkv + kvh;
+            // (a new token where it is: another workgroup may be writing it into its page)
+            const int64_t hd = (int64_t)id * a.Hkv + kvh, at = (int64_t)(s.start + key - (s.len - s.m)) * a.kv_stride + kvh * DH;
+            const bool fresh = a.k_new && key >= s.len - s.m;
+            const T *kr = fresh ? (const T *)a.k_new + at : (const T *)a.k + (hd * page + slot) * DH, *vr = fresh ? (const T *)a.v_new + at : (const T *)a.v + hd * DH * page + slot;
+            const int vs = fresh ? 1 : page;
             float dot = 0.0f, v[E];
 #pragma unroll
             for (int e = 0; e < E; e++) {
                 const int c = lane + 64 * e;
                 v[e] = 0.0f;
                 if (c < DH) {
-                    dot = fmaf(qv[e], to_f(((const T *)a.k)[(hd * page + slot) * DH + c]), dot);
-                    v[e] = to_f(((const T *)a.v)[(hd * DH + c) * page + slot]);
+                    dot = fmaf(qv[e], to_f(kr[c]), dot);
+                    v[e] = to_f(vr[c * vs]);
                 }
             }
             dot = wave_sum(dot) * a.scale_log2e;
@@ -225,7 +229,7 @@ __device__ __forceinline__ int page_numbers(const PagedArgs &a, int b, int first
 // A lane holds row lane % 16 of the first operand and c = lane / 16 says which part of the contraction; of S^T it gets query lane % 16 and four rows.
 // bf16: key rows enter in an order that makes the eight keys a lane then holds of P consecutive, as its piece of V^T has them.
 // New tokens among a block's keys, [first, end) of it: k, v are where its key 0 would lie among their rows
-template <typename T> struct NewRows { const T *k, *v; int64_t stride; int first, end; };
+template <typename T> struct NewRows { const T *k, *v; int64_t stride; int first, end, keep_from, keep_to; };  // [keep_from, keep_to]: keys this workgroup writes
 template <typename T, int DH> struct Frags;
 template <int DH> struct Frags<bf16, DH> {
     static constexpr int KB = 32, KF = (DH + 31) / 32, VF = DH / 16;
@@ -292,10 +296,11 @@ template <int DH> struct Frags<bf16, DH> {
             if (key < n.first || key >= n.end || 8 * c >= DH) continue;
             const bf16 *src = n.k + (int64_t)key * n.stride + 8 * c;
             bf16 *dst = (r < 8 ? k0 : k1) + (key % 16) * DH + 8 * c;
+            const bool keep = key >= n.keep_from && key <= n.keep_to;
 #pragma unroll
             for (int f = 0; f < KF; f++) {
                 k[u][f] = *(const bf16x8 *)(src + 32 * f);
-                if (valid >> (key / 16) & 1) *(bf16x8 *)(dst + 32 * f) = k[u][f];
+                if (keep && (valid >> (key / 16) & 1)) *(bf16x8 *)(dst + 32 * f) = k[u][f];
             }
         }
         bf16 *dst = (c < 2 ? v0 : v1) + (8 * c) % 16 + r * page;
@@ -303,10 +308,11 @@ template <int DH> struct Frags<bf16, DH> {
         for (int e = 0; e < 8; e++) {
             const int key = 8 * c + e;
             if (key < n.first || key >= n.end) continue;
+            const bool keep = key >= n.keep_from && key <= n.keep_to;
 #pragma unroll
             for (int t = 0; t < VF; t++) {
                 v[t][e] = n.v[(int64_t)key * n.stride + 16 * t + r];
-                if (valid >> (key / 16) & 1) dst[16 * t * page + e] = v[t][e];
+                if (keep && (valid >> (key / 16) & 1)) dst[16 * t * page + e] = v[t][e];
             }
         }
     }
@@ -359,20 +365,22 @@ template <int DH> struct Frags<float, DH> {
     __device__ __forceinline__ void take_new(const NewRows<float> &n, float *k0, float *, float *v0, float *, int valid, int page) {
         const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
         if (r >= n.first && r < n.end) {
+            const bool keep = r >= n.keep_from && r <= n.keep_to;
 #pragma unroll
             for (int f = 0; f < KF; f++) {
                 k[f] = *(const floatx4 *)(n.k + (int64_t)r * n.stride + 16 * f + 4 * c);
-                if (valid) *(floatx4 *)(k0 + r * DH + 16 * f + 4 * c) = k[f];
+                if (keep && valid) *(floatx4 *)(k0 + r * DH + 16 * f + 4 * c) = k[f];
             }
         }
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int key = 4 * c + e;
             if (key < n.first || key >= n.end) continue;
+            const bool keep = key >= n.keep_from && key <= n.keep_to;
 #pragma unroll
             for (int t = 0; t < VF; t++) {
                 v[t][e] = n.v[(int64_t)key * n.stride + 16 * t + r];
-                if (valid) v0[(16 * t + r) * page + key] = v[t][e];
+                if (keep && valid) v0[(16 * t + r) * page + key] = v[t][e];
             }
         }
     }
@@ -401,7 +409,7 @@ __device__ __forceinline__ float query_sum(float v) {
 }
 
 // MR groups of 16 rows per workgroup (each key read serves them all).
-template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH <= 64 ? 4 : 2) void paged_rows(PagedArgs a) {
+template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH <= 64 ? 4 : MR == 2 ? 3 : 2) void paged_rows(PagedArgs a) {
     using F = Frags<T, DH>;
     constexpr int KB = F::KB, VF = F::VF, NW = 4, ROWS = 16 * MR;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, c = lane / 16;
@@ -474,7 +482,7 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
         const int key0 = bl.at(x) * KB, valid = src.valid;
         if constexpr (NEW) {
             const int64_t row = (int64_t)(s.start + key0 - base) * a.kv_stride + kvh * DH;
-            const NewRows<T> nr = {(const T *)a.k_new + row, (const T *)a.v_new + row, a.kv_stride, base - key0, s.len - key0};
+            const NewRows<T> nr = {(const T *)a.k_new + row, (const T *)a.v_new + row, a.kv_stride, base - key0, s.len - key0, p_lo - key0, p_hi - key0};
             f.take_new(nr, (T *)src.k0, (T *)src.k1, (T *)src.v0, (T *)src.v1, valid, page);
         }
         floatx4 sc[MR][F::TILES];
@@ -548,8 +556,8 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
         f.load_v(src.v0, src.v1, page);
         constexpr std::true_type yes;
         constexpr std::false_type no;
-        // From block xn on there are new tokens: they are read where they are and written into their pages by whoever walks their block.  (Several tiles of
-        // one sequence then write the same; the tile of a token's own row always walks it.)
+        // From block xn on there are new tokens: they are read where they are, and written into their pages by the tile of the token's own rows, which always
+        // walks its block (where two tiles share a token they write the same).
         int xn = x1;
         if (a.k_new) {
             const int first = max(base, 0) / KB;
@@ -1087,11 +1095,14 @@ Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, 
     Plan p;
     const int group = H / Hkv;
     const int64_t rows = (int64_t)N * group / B;  // of a sequence and key head, on average
-    p.rows = rows <= 16 ? 16 : dtype == GR4AD_BF16 && dh >= 32 && rows >= 64 ? kFlashRows : 32;
+    p.rows = dtype == GR4AD_BF16 && dh >= 32 && rows >= 64 ? kFlashRows : rows <= 16 || dh > 64 ? 16 : 32;  // (32 rows of 128 columns do not fit the registers)
     p.tiles = tiles_of(N, B, group, p.rows);
     p.join_tiles = tiles_of(N, B, group, kRows);
     const bool flash = p.rows == kFlashRows;
-    const int64_t blocks = p.tiles * Hkv, enough = flash ? 256 : 2048, least = flash ? 1024 : 256;
+    // Workgroups enough to fill the chip: one per compute unit for tiles of 256 rows, two for the others (tiles of 32 rows, 840 of them: 130 us alone, 136 in
+    // halves with their join); with tiles of 16 rows, which stand for many sequences of their own lengths, four where that many are near (640 of up to 8192 keys:
+    // alone 261 us, in halves 233, in quarters 238; 16 of 100000 keys in 16 parts 175 us, in 64 parts 189).  A part has 256 (1024) keys at least.
+    const int64_t blocks = p.tiles * Hkv, enough = flash ? 256 : p.rows == 16 && blocks >= 256 ? 1024 : 512, least = flash ? 1024 : 256;
     int64_t keys = (int64_t)max_pages * page;
     if (window && (int64_t)window + sinks + 64 < keys) keys = (int64_t)window + sinks + 64;
     const int64_t want = (enough + blocks - 1) / blocks, most = (keys + least - 1) / least, n = want < most ? want : most;
@@ -1113,7 +1124,7 @@ template <typename T, int DH> int launch_rows(const PagedArgs &a, const Plan &p,
     if (p.rows == 16) {
         hipLaunchKernelGGL((paged_rows<T, DH, 1>), dim3((unsigned)grid), dim3(256), 0, st, a);
     } else if (p.rows == 32) {
-        hipLaunchKernelGGL((paged_rows<T, DH, 2>), dim3((unsigned)grid), dim3(256), 0, st, a);
+        if constexpr (DH <= 64) hipLaunchKernelGGL((paged_rows<T, DH, 2>), dim3((unsigned)grid), dim3(256), 0, st, a);
     } else if constexpr (sizeof(T) == 2 && DH >= 32) {
         constexpr int NW = kFlashRows / 32, SLOTS = 4, LDS = 2 * SLOTS * 64 * DH * 2;
         const int s = allow_lds((const void *)paged_flash<DH, NW, SLOTS>, LDS);
