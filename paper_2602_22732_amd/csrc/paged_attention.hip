@@ -7,7 +7,7 @@
 // The cache: keys [page][H_kv][slot][dh], values transposed [page][H_kv][dh][slot], so that a page of one head is one stretch of memory
 // and both operands of the two products, S^T = K Q^T and O^T = V^T P^T, are read along their contraction in 16-byte pieces.
 //
-//  * paged_append<T>        new keys and values into their pages.
+//  * paged_append<T, DH>    new keys and values into their pages (ahead of paged_flash; the others take them where they are).
 //  * paged_rows<T, DH>      16 rows (token, head of the group) of one (sequence, key head) per workgroup, whose wavefronts walk
 //                           stretches of the keys of their own; operands go from memory to registers.
 //  * paged_flash<DH>        128 rows per workgroup, keys and values staged in LDS (bf16).
@@ -104,7 +104,12 @@ template <typename F> __device__ __forceinline__ bool find_longest_first(const P
 __device__ __forceinline__ int page_of(const PagedArgs &a, int b, int key) { return a.table[(int64_t)b * a.max_pages + (key >> a.page_shift)]; }
 
 // New keys and values of 64 positions (counted from the sequence's first) and one key head.  Positions on a page number that does not exist are left out.
-template <typename T> __global__ __launch_bounds__(256) void paged_append(PagedArgs a, int dh) {
+// Both are read in 16-byte pieces; the values turn in LDS and leave in pieces of 8 positions (one by one where not all of them are new): written one by one
+// from their rows they took most of 51 us for 4048 tokens of 8 heads of 128 columns.
+template <typename T, int DH> __global__ __launch_bounds__(256) void paged_append(PagedArgs a) {
+    constexpr int P = 16 / sizeof(T), CH = DH / P;  // values of a piece, pieces of a row
+    typedef T Piece __attribute__((ext_vector_type(P)));
+    __shared__ T turn[kAppendKeys][DH + 2];
     Sequence s;
     const int64_t t = blockIdx.x / a.Hkv;
     const int h = blockIdx.x % a.Hkv;
@@ -113,17 +118,34 @@ template <typename T> __global__ __launch_bounds__(256) void paged_append(PagedA
         return m > 0 && len > first ? (len - 1) / kAppendKeys - first / kAppendKeys + 1 : 0;
     };
     if (!find_sequence(a, t, tiles, s)) return;
-    const int base = s.len - s.m, first = max(base, 0);
-    const int k0 = max((first / kAppendKeys + s.tile) * kAppendKeys, first), k1 = min((first / kAppendKeys + s.tile + 1) * kAppendKeys, s.len);
+    const int base = s.len - s.m, tile0 = (max(base, 0) / kAppendKeys + s.tile) * kAppendKeys, k0 = max(tile0, max(base, 0)), k1 = min(tile0 + kAppendKeys, s.len);
     const int page = 1 << a.page_shift;
-    for (int i = threadIdx.x; i < (k1 - k0) * dh; i += 256) {
-        const int key = k0 + i / dh, c = i % dh;
-        const int id = page_of(a, s.b, key), slot = key & (page - 1);
+    for (int i = threadIdx.x; i < (k1 - k0) * CH; i += 256) {
+        const int key = k0 + i / CH, c = i % CH * P, id = page_of(a, s.b, key);
+        const int64_t src = (int64_t)(s.start + key - base) * a.kv_stride + h * DH + c;
+        const Piece k = *(const Piece *)((const T *)a.k_new + src), v = *(const Piece *)((const T *)a.v_new + src);
+        if (id >= 0 && id < a.n_pages) *(Piece *)((T *)a.k + (((int64_t)id * a.Hkv + h) * page + (key & (page - 1))) * DH + c) = k;
+#pragma unroll
+        for (int e = 0; e < P; e++) turn[key - tile0][c + e] = v[e];
+    }
+    __syncthreads();
+    constexpr int G = kAppendKeys / P;  // groups of P positions (P divides the page: on one of them)
+    for (int i = threadIdx.x; i < G * DH; i += 256) {
+        const int g = i % G * P, c = i / G, key = tile0 + g;
+        if (key + P <= k0 || key >= k1) continue;
+        const int id = page_of(a, s.b, key);
         if (id < 0 || id >= a.n_pages) continue;
-        const int64_t head = (int64_t)id * a.Hkv + h;
-        const int64_t src = (int64_t)(s.start + key - base) * a.kv_stride + h * dh + c;
-        ((T *)a.k)[(head * page + slot) * dh + c] = ((const T *)a.k_new)[src];
-        ((T *)a.v)[(head * dh + c) * page + slot] = ((const T *)a.v_new)[src];
+        T *dst = (T *)a.v + (((int64_t)id * a.Hkv + h) * DH + c) * page + (key & (page - 1));
+        if (key >= k0 && key + P <= k1) {
+            Piece v;
+#pragma unroll
+            for (int e = 0; e < P; e++) v[e] = turn[g + e][c];
+            *(Piece *)dst = v;
+        } else {
+#pragma unroll
+            for (int e = 0; e < P; e++)
+                if (key + e >= k0 && key + e < k1) dst[e] = turn[g + e][c];
+        }
     }
 }
 
@@ -965,17 +987,21 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
             }
         };
         // tile x, whose scores are in c; the next tile's go to n
+        const bool idle = W0 >= R1;  // a wavefront without rows loads for the others
         auto step = [&](int x, Scores &c, Scores &n) {
             arrive(x);
+            if (!idle) {
             scores(yes, yes, at_tile(k_lane, after(1)), n, c);
             mask(bl.at(x + 1) * KT, (unsigned)(valid >> 8) & 0xFF, n);
             values(yes, at_tile(v_lane, slot), c, n);
             follow();
+            }
             valid >>= 8;
             slot = after(1);
         };
         auto last = [&](int x, Scores &c) {
             arrive(x);
+            if (idle) return;
             scores(no, yes, 0u, c, c);
             values(no, at_tile(v_lane, slot), c, c);
         };
@@ -1081,7 +1107,7 @@ int shift_of(int page) {
     return s;
 }
 
-constexpr int kFlashRows = 256;
+constexpr int kFlashRows = 256, kHalfFlashRows = 128;
 
 // bound of the tiles of `rows` rows, of one key head
 int64_t tiles_of(int N, int B, int group, int rows) {
@@ -1090,19 +1116,27 @@ int64_t tiles_of(int N, int B, int group, int rows) {
 }
 
 // rows: of a tile: 16 or 32 (paged_rows), or 256 that share staged keys (paged_flash).  nsplit: workgroups that share a tile's keys.
-struct Plan { int rows; int64_t tiles, join_tiles; int nsplit; size_t bytes; };
+struct Plan {
+    int rows;
+    int64_t tiles, join_tiles;
+    int nsplit;
+    size_t bytes;
+    bool flash() const { return rows >= kHalfFlashRows; }
+};
 Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, int max_pages, int window, int sinks) {
     Plan p;
     const int group = H / Hkv;
-    const int64_t rows = (int64_t)N * group / B;  // of a sequence and key head, on average
-    p.rows = dtype == GR4AD_BF16 && dh >= 32 && rows >= 64 ? kFlashRows : rows <= 16 || dh > 64 ? 16 : 32;  // (32 rows of 128 columns do not fit the registers)
+    const int64_t rows = ceil_div64((int64_t)N * group, B);  // of a sequence and key head, on average
+    if (dtype == GR4AD_BF16 && dh >= 32 && (rows >= 48 || (dh == 128 && rows > 16))) p.rows = rows > 128 ? kFlashRows : kHalfFlashRows;
+    else p.rows = rows <= 16 || dh > 64 ? 16 : 32;  // (32 rows of 128 columns do not fit the registers)
     p.tiles = tiles_of(N, B, group, p.rows);
     p.join_tiles = tiles_of(N, B, group, kRows);
-    const bool flash = p.rows == kFlashRows;
-    // Workgroups enough to fill the chip: one per compute unit for tiles of 256 rows, two for the others (tiles of 32 rows, 840 of them: 130 us alone, 136 in
-    // halves with their join); with tiles of 16 rows, which stand for many sequences of their own lengths, four where that many are near (640 of up to 8192 keys:
-    // alone 261 us, in halves 233, in quarters 238; 16 of 100000 keys in 16 parts 175 us, in 64 parts 189).  A part has 256 (1024) keys at least.
-    const int64_t blocks = p.tiles * Hkv, enough = flash ? 256 : p.rows == 16 && blocks >= 256 ? 1024 : 512, least = flash ? 1024 : 256;
+    const bool flash = p.flash();
+    // Workgroups enough to fill the chip (counted as if all sequences had the same number of rows): one per compute unit for tiles of 256 rows, two for the
+    // others (tiles of 32 rows, 840 of them: 130 us alone, 136 in halves with their join); with tiles of 16 rows, which stand for many sequences of their
+    // own lengths, four where that many are near (512 of up to 8192 keys: alone 261 us, in halves 233, in quarters 238; 16 of 100000 keys in 16 parts 175 us, in
+    // 64 parts 189).  A part has 256 (1024) keys at least.
+    const int64_t blocks = (int64_t)B * ceil_div64(rows, p.rows) * Hkv, enough = p.rows == kFlashRows ? 256 : p.rows == 16 && blocks >= 256 ? 1024 : 512, least = flash ? 1024 : 256;
     int64_t keys = (int64_t)max_pages * page;
     if (window && (int64_t)window + sinks + 64 < keys) keys = (int64_t)window + sinks + 64;
     const int64_t want = (enough + blocks - 1) / blocks, most = (keys + least - 1) / least, n = want < most ? want : most;
@@ -1118,6 +1152,16 @@ int allow_lds(const void *kernel, int bytes) {
     return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess ? GR4AD_OK : GR4AD_EHIP;
 }
 
+template <int DH, int NW, int SLOTS> int launch_flash(const PagedArgs &a, unsigned grid, hipStream_t st) {
+    constexpr int LDS = 2 * SLOTS * 64 * DH * 2;
+    if (LDS > 65536) {
+        const int s = allow_lds((const void *)paged_flash<DH, NW, SLOTS>, LDS);
+        if (s) return s;
+    }
+    hipLaunchKernelGGL((paged_flash<DH, NW, SLOTS>), dim3(grid), dim3(NW * 64), LDS, st, a);
+    return GR4AD_OK;
+}
+
 template <typename T, int DH> int launch_rows(const PagedArgs &a, const Plan &p, hipStream_t st) {
     const int64_t grid = p.tiles * a.Hkv * a.nsplit, joined = p.join_tiles * a.Hkv * kRows;
     if (grid > 0x7fffffffLL || joined > 0x7fffffffLL) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: %d rows of %d heads", a.N, a.H);
@@ -1126,10 +1170,9 @@ template <typename T, int DH> int launch_rows(const PagedArgs &a, const Plan &p,
     } else if (p.rows == 32) {
         if constexpr (DH <= 64) hipLaunchKernelGGL((paged_rows<T, DH, 2>), dim3((unsigned)grid), dim3(256), 0, st, a);
     } else if constexpr (sizeof(T) == 2 && DH >= 32) {
-        constexpr int NW = kFlashRows / 32, SLOTS = 4, LDS = 2 * SLOTS * 64 * DH * 2;
-        const int s = allow_lds((const void *)paged_flash<DH, NW, SLOTS>, LDS);
+        // (half the rows: two workgroups share a compute unit and its LDS)
+        const int s = p.rows == kFlashRows ? launch_flash<DH, kFlashRows / 32, 4>(a, (unsigned)grid, st) : launch_flash<DH, kHalfFlashRows / 32, DH == 128 ? 2 : 4>(a, (unsigned)grid, st);
         if (s) return s;
-        hipLaunchKernelGGL((paged_flash<DH, NW, SLOTS>), dim3((unsigned)grid), dim3(NW * 64), LDS, st, a);
     }
     GR4AD_LAUNCH_CHECK();
     if (a.nsplit > 1) {
@@ -1195,14 +1238,16 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
     PagedArgs a = {q, q_stride, k_new, v_new, kv_stride, q_start, seq_len, c.page_table, c.k_pages, c.v_pages, c.n_pages, shift_of(c.page_size), c.max_pages, B, N, H, c.H_kv,
                    H / c.H_kv, scale * 1.4426950408889634f, window > kMostKeys ? kMostKeys : window, sinks > kMostKeys ? kMostKeys : sinks, out, (float *)workspace, p.nsplit};
     const int e = dtype == GR4AD_BF16 ? 2 : 4;
-    if (k_new && p.rows == kFlashRows) {  // (the smaller tiles take the new tokens where they are)
+    if (k_new && p.flash()) {  // (the smaller tiles take the new tokens where they are)
         int64_t tiles = (int64_t)N / kAppendKeys + 2 * (int64_t)B;
         if (tiles > N) tiles = N;
         const int64_t grid = tiles * c.H_kv;
         if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
         ProfScope ps(KC_PAGED_APPEND, st, 0.0, 4.0 * N * c.H_kv * c.dh * e);
-        if (dtype == GR4AD_BF16) hipLaunchKernelGGL(paged_append<bf16>, dim3((unsigned)grid), dim3(256), 0, st, a, c.dh);
-        else hipLaunchKernelGGL(paged_append<float>, dim3((unsigned)grid), dim3(256), 0, st, a, c.dh);
+        // (tiles of many rows: bf16, widths from 32 on)
+        if (c.dh == 32) hipLaunchKernelGGL((paged_append<bf16, 32>), dim3((unsigned)grid), dim3(256), 0, st, a);
+        else if (c.dh == 64) hipLaunchKernelGGL((paged_append<bf16, 64>), dim3((unsigned)grid), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((paged_append<bf16, 128>), dim3((unsigned)grid), dim3(256), 0, st, a);
         GR4AD_LAUNCH_CHECK();
     }
     // lengths lie on the device: counted on all pages of every sequence, an upper bound
