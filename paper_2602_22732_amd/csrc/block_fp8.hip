@@ -258,6 +258,138 @@ template <int TM, int TN> __global__ __launch_bounds__(256) void gemm_block_tile
         for (int j = 0; j < GN; j++) store4(g, m0 + wm * WM + 16 * i + r, n0 + wn * WN + 16 * j + 4 * c, acc[i][j]);
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// Large products: 256 x 256 tiles of C on 8 wavefronts (2 x 4, 128 x 64 each), one workgroup per compute unit.  A block of K is a half-tile of A and one of
+// W (256 rows x 128 bytes), which travel from memory to LDS without passing registers: three slots for A, two for W (160 KB), so that a block's A has two
+// blocks' time to land and its W one.  Chunk p of row r lies at p ^ (r / 2 % 8), applied where it is read from memory.
+// Per block and wavefront 24 KB of fragments feed 32 MFMAs; each one's sums are scaled into the accumulators while the next ones run.
+// ---------------------------------------------------------------------------------------------------------------------
+__device__ __attribute__((aligned(16))) uint8_t zero_chunk[16];  // stands for the chunks past the end of a row
+
+constexpr int kRing = 256;  // rows of a half-tile
+__global__ __launch_bounds__(512, 2) void gemm_block_ring(BlockGemm g, int tiles_m, int tiles_n) {
+    extern __shared__ intx4 smem[];  // 3 + 2 half-tiles of 2048 chunks
+    constexpr int HALF = kRing * 8;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, c = lane / 16, wm = wave / 4, wn = wave % 4;
+    // Every XCD (workgroup id % 8) owns a contiguous range of tiles, 8 row blocks deep and then along the columns, so that its workgroups share operands in its L2
+    const int total = tiles_m * tiles_n, per = (total + 7) / 8, l = (blockIdx.x % 8) * per + blockIdx.x / 8;
+    if (blockIdx.x / 8 >= per || l >= total) return;
+    const int deep = 8 * tiles_n, grp = l / deep, in = l - grp * deep, rows_here = min(8, tiles_m - grp * 8), col = in / rows_here;
+    const int m0 = (grp * 8 + in - col * rows_here) * kRing, n0 = col * kRing;
+
+    // loads: load j of a wavefront fills rows (4 wave + j) 8 .. + 7 of a half-tile, lane -> row lane / 8, place lane % 8; which chunk that is changes with j's parity
+    const int row0 = wave * 32 + lane / 8, ch0 = (lane % 8) ^ ((lane / 8) >> 1);
+    const uint8_t *base_a = g.A + (int64_t)m0 * g.K, *base_w = g.W + (int64_t)n0 * g.K;
+    const int last_a = g.M - 1 - m0, last_w = g.N - 1 - n0;
+    unsigned a_off[4], w_off[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) {  // (rows past the edge re-read the last one)
+        const unsigned k = (unsigned)(ch0 ^ ((j & 1) * 4)) * 16;
+        a_off[j] = (unsigned)min(row0 + 8 * j, last_a) * (unsigned)g.K + k;
+        w_off[j] = (unsigned)min(row0 + 8 * j, last_w) * (unsigned)g.K + k;
+    }
+    auto piece = [&](const uint8_t *base, unsigned off, int kb, int slot, int j) {
+        const uint8_t *src = base + kb * 128 + off;
+        if (kb * 128 + 128 > g.K && kb * 128 + (ch0 ^ ((j & 1) * 4)) * 16 >= g.K) src = zero_chunk;
+        __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)src, (void __attribute__((address_space(3))) *)(smem + slot * HALF + (wave * 4 + j) * 64), 16, 0, 0);
+    };
+    typedef const __attribute__((address_space(3))) intx4 *LdsChunk;
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    const unsigned swz = (unsigned)(c ^ ((r >> 1) & 7)) * 16;  // chunk c of row r of 16; chunk c + 4 lies 64 bytes off (their bit 2 differs)
+    const unsigned a_lane = lds0 + (unsigned)(wm * 128 + r) * 128 + swz, w_lane = lds0 + 3 * HALF * 16 + (unsigned)(wn * 64 + r) * 128 + swz;
+    auto frag = [&](unsigned at, int i) { return join8(*((LdsChunk)at + i * 128), *((LdsChunk)(at ^ 64u) + i * 128)); };
+
+    // scales of a block: a row's in its lane (8 row groups), the weights' for 64 successive blocks one per lane
+    const float *sa = g.sa + m0;
+    const int m_lane = wm * 128 + r;
+    auto row_scales = [&](float (&s)[8], const float *of) {
+        int at = m_lane;
+        asm volatile("" : "+v"(at));  // (the places are formed here and not kept in registers over the loop)
+#pragma unroll
+        for (int i = 0; i < 8; i++) s[i] = of[min(at + 16 * i, last_a)];
+    };
+    const int nblk = min((n0 + wn * 64) / 128, g.wb - 1);
+    float sw64 = 0.0f;
+    auto weight_scale = [&](int kb) {
+        if (kb % 64 == 0) {
+            const float *src = g.sw + (int64_t)min(kb + lane, g.nb - 1) * g.wb + nblk;
+            asm volatile("global_load_dword %0, %1, off\n\ts_waitcnt vmcnt(0)" : "=&v"(sw64) : "v"(src) : "memory");
+        }
+        return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sw64), kb % 64));
+    };
+    floatx4 acc[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    float s_now[8], s_next[8];
+    const int nb = g.nb;
+    row_scales(s_next, sa);
+#pragma unroll
+    for (int j = 0; j < 4; j++) piece(base_a, a_off[j], 0, 0, j);
+#pragma unroll
+    for (int j = 0; j < 4; j++) piece(base_w, w_off[j], 0, 3, j);
+#pragma unroll
+    for (int j = 0; j < 4; j++) piece(base_a, a_off[j], min(1, nb - 1), 1, j);
+    int a_slot = 0;
+    for (int kb = 0; kb < nb; kb++) {
+        const float sw = weight_scale(kb);
+        // all but A of the next block has landed (the compiler sees this wait and knows that the scales have); the block before is read out
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(4 | 7 << 4);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 8; i++) s_now[i] = s_next[i];
+        const int next = min(kb + 1, nb - 1), after = min(kb + 2, nb - 1), a_free = a_slot == 0 ? 2 : a_slot - 1, w_slot = kb & 1;
+        sa += next > kb ? g.M : 0;
+        row_scales(s_next, sa);
+        const unsigned at_a = a_lane + (unsigned)a_slot * HALF * 16, at_w = w_lane + (unsigned)w_slot * HALF * 16;
+        intx8 wf[4], af[2];
+        af[0] = frag(at_a, 0);
+#pragma unroll
+        for (int j = 0; j < 4; j++) wf[j] = frag(at_w, j);
+        constexpr int SKEW = 3;  // MFMAs between one and the use of its sums
+        floatx4 p[SKEW + 1];
+        float s = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 32 + SKEW; t++) {
+            const int i = t / 4, j = t % 4, u = t - SKEW;
+            if (t < 32) {
+                if (j == 0 && i < 7) af[(i + 1) & 1] = frag(at_a, i + 1);
+                p[t % (SKEW + 1)] = mfma_block(wf[j], af[i & 1]);
+                // (the slots that block kb - 1 left take W of the next block and A of the one after, a load at a time)
+                if (j == 2) {
+                    if (i < 4) piece(base_w, w_off[i], next, 3 + (w_slot ^ 1), i);
+                    else piece(base_a, a_off[i - 4], after, a_free, i - 4);
+                }
+            }
+            if (u >= 0) {
+                if (u % 4 == 0) s = s_now[u / 4] * sw;
+#pragma unroll
+                for (int v = 0; v < 4; v++) acc[u / 4][u % 4][v] = fmaf(p[u % (SKEW + 1)][v], s, acc[u / 4][u % 4][v]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        a_slot = a_slot == 2 ? 0 : a_slot + 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (loads in flight own their slots)
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) store4(g, m0 + wm * 128 + 16 * i + r, n0 + wn * 64 + 16 * j + 4 * c, acc[i][j]);
+}
+
+int launch_ring(const BlockGemm &g, hipStream_t st) {
+    constexpr int LDS = 5 * kRing * 128;
+    if (hipFuncSetAttribute((const void *)gemm_block_ring, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return GR4AD_EHIP;
+    const int64_t tiles_m = ceil_div64(g.M, kRing), tiles_n = ceil_div64(g.N, kRing), grid = (tiles_m * tiles_n + 7) / 8 * 8;
+    if (grid > 0x3fffffffLL) return GR4AD_EUNSUPPORTED;
+    hipLaunchKernelGGL(gemm_block_ring, dim3((unsigned)grid), dim3(512), LDS, st, g, (int)tiles_m, (int)tiles_n);
+    GR4AD_LAUNCH_CHECK();
+    return GR4AD_OK;
+}
+
 template <int TM, int TN> int launch_tile(const BlockGemm &g, hipStream_t st) {
     const int64_t grid = ceil_div64(g.M, TM) * ceil_div64(g.N, TN);
     if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
@@ -276,6 +408,8 @@ int launch_block_gemm(const BlockGemm &g, hipStream_t st) {
         GR4AD_LAUNCH_CHECK();
         return GR4AD_OK;
     }
+    const bool aligned = g.K % 16 == 0 && (uintptr_t)g.A % 16 == 0 && (uintptr_t)g.W % 16 == 0;
+    if (aligned && ceil_div64(g.M, kRing) * ceil_div64(g.N, kRing) >= 192) return launch_ring(g, st);
     if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) < 256) return launch_tile<64, 64>(g, st);
     return launch_tile<128, 128>(g, st);
 }
