@@ -331,37 +331,51 @@ __global__ __launch_bounds__(512, 2) void gemm_block_ring(BlockGemm g, int tiles
     for (int j = 0; j < 4; j++) piece(base_w, w_off[j], 0, 3, j);
 #pragma unroll
     for (int j = 0; j < 4; j++) piece(base_a, a_off[j], min(1, nb - 1), 1, j);
-    int a_slot = 0;
-    for (int kb = 0; kb < nb; kb++) {
-        const float sw = weight_scale(kb);
-        // all but A of the next block has landed (the compiler sees this wait and knows that the scales have); the block before is read out
+    // All but A of the block after next has landed (the compiler sees this wait and knows that the scales have), and everybody has read the block before.
+    auto meet = [&]() {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(4 | 7 << 4);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-#pragma unroll
-        for (int i = 0; i < 8; i++) s_now[i] = s_next[i];
-        const int next = min(kb + 1, nb - 1), after = min(kb + 2, nb - 1), a_free = a_slot == 0 ? 2 : a_slot - 1, w_slot = kb & 1;
-        sa += next > kb ? g.M : 0;
-        row_scales(s_next, sa);
-        const unsigned at_a = a_lane + (unsigned)a_slot * HALF * 16, at_w = w_lane + (unsigned)w_slot * HALF * 16;
-        intx8 wf[4], af[2];
+    };
+    intx8 wf[4], af[3];  // fragments: the block's columns, and row groups i % 3
+    int a_slot = 0, a_next = 1;
+    meet();
+    {
+        const unsigned at_a = a_lane, at_w = w_lane;
         af[0] = frag(at_a, 0);
 #pragma unroll
         for (int j = 0; j < 4; j++) wf[j] = frag(at_w, j);
-        constexpr int SKEW = 3;  // MFMAs between one and the use of its sums
+        af[1] = frag(at_a, 1);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) s_now[i] = s_next[i];
+    constexpr int SKEW = 3;  // MFMAs between one and the use of its sums
+    for (int kb = 0; kb < nb; kb++) {
+        const float sw = weight_scale(kb);
+        const int next = min(kb + 1, nb - 1), after = min(kb + 2, nb - 1), a_free = 3 - a_slot - a_next, w_next = (kb & 1) ^ 1;
+        sa += next > kb ? g.M : 0;
+        row_scales(s_next, sa);
+        const unsigned at_a = a_lane + (unsigned)a_slot * HALF * 16;
+        const unsigned next_a = a_lane + (unsigned)a_next * HALF * 16, next_w = w_lane + (unsigned)w_next * HALF * 16;
         floatx4 p[SKEW + 1];
         float s = 0.0f;
 #pragma unroll
         for (int t = 0; t < 32 + SKEW; t++) {
             const int i = t / 4, j = t % 4, u = t - SKEW;
+            if (t == 28) {  // the last row group is in registers: on to the next block, whose fragments are read under this one's last MFMAs
+                meet();
+                af[(8 + 0) % 3] = frag(next_a, 0);
+            }
             if (t < 32) {
-                if (j == 0 && i < 7) af[(i + 1) & 1] = frag(at_a, i + 1);
-                p[t % (SKEW + 1)] = mfma_block(wf[j], af[i & 1]);
+                if (j == 0 && i < 6) af[(i + 2) % 3] = frag(at_a, i + 2);
+                p[t % (SKEW + 1)] = mfma_block(wf[j], af[i % 3]);
+                if (i == 7) wf[j] = frag(next_w, j);
                 // (the slots that block kb - 1 left take W of the next block and A of the one after, a load at a time)
-                if (j == 2) {
-                    if (i < 4) piece(base_w, w_off[i], next, 3 + (w_slot ^ 1), i);
-                    else piece(base_a, a_off[i - 4], after, a_free, i - 4);
+                if (t % 3 == 2 && t / 3 < 8) {
+                    const int q = t / 3;
+                    if (q < 4) piece(base_w, w_off[q], next, 3 + w_next, q);
+                    else piece(base_a, a_off[q - 4], after, a_free, q - 4);
                 }
             }
             if (u >= 0) {
@@ -371,7 +385,13 @@ __global__ __launch_bounds__(512, 2) void gemm_block_ring(BlockGemm g, int tiles
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        a_slot = a_slot == 2 ? 0 : a_slot + 1;
+        // row groups 0 and 1 of the next block belong into places 0 and 1 (group 7 was in place 1, 8 is in place 2)
+        af[0] = af[2];
+        af[1] = frag(next_a, 1);
+#pragma unroll
+        for (int i = 0; i < 8; i++) s_now[i] = s_next[i];
+        a_slot = a_next;
+        a_next = a_free;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (loads in flight own their slots)
 #pragma unroll
