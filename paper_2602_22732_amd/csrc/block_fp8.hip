@@ -267,7 +267,8 @@ template <int TM, int TN> __global__ __launch_bounds__(256) void gemm_block_tile
 __device__ __attribute__((aligned(16))) uint8_t zero_chunk[16];  // stands for the chunks past the end of a row
 
 constexpr int kRing = 256;  // rows of a half-tile
-__global__ __launch_bounds__(512, 2) void gemm_block_ring(BlockGemm g, int tiles_m, int tiles_n) {
+// RAGGED: K is no multiple of 128; EDGE: M is no multiple of 256
+template <bool RAGGED, bool EDGE> __global__ __launch_bounds__(512, 2) void gemm_block_ring(BlockGemm g, int tiles_m, int tiles_n) {
     extern __shared__ intx4 smem[];  // 3 + 2 half-tiles of 2048 chunks
     constexpr int HALF = kRing * 8;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, c = lane / 16, wm = wave / 4, wn = wave % 4;
@@ -288,10 +289,13 @@ __global__ __launch_bounds__(512, 2) void gemm_block_ring(BlockGemm g, int tiles
         a_off[j] = (unsigned)min(row0 + 8 * j, last_a) * (unsigned)g.K + k;
         w_off[j] = (unsigned)min(row0 + 8 * j, last_w) * (unsigned)g.K + k;
     }
-    auto piece = [&](const uint8_t *base, unsigned off, int kb, int slot, int j) {
-        const uint8_t *src = base + kb * 128 + off;
-        if (kb * 128 + 128 > g.K && kb * 128 + (ch0 ^ ((j & 1) * 4)) * 16 >= g.K) src = zero_chunk;
+    auto dma = [&](const uint8_t *src, int slot, int j) {
         __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)src, (void __attribute__((address_space(3))) *)(smem + slot * HALF + (wave * 4 + j) * 64), 16, 0, 0);
+    };
+    auto piece = [&](const uint8_t *base, unsigned off, int kb, int slot, int j) {
+        const uint8_t *at = base + kb * 128;  // (uniform: a whole block's load adds nothing per lane)
+        if constexpr (!RAGGED) dma(at + off, slot, j);
+        else dma(kb * 128 + (ch0 ^ ((j & 1) * 4)) * 16 < g.K ? at + off : zero_chunk, slot, j);
     };
     typedef const __attribute__((address_space(3))) intx4 *LdsChunk;
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
@@ -301,12 +305,17 @@ __global__ __launch_bounds__(512, 2) void gemm_block_ring(BlockGemm g, int tiles
 
     // scales of a block: a row's in its lane (8 row groups), the weights' for 64 successive blocks one per lane
     const float *sa = g.sa + m0;
-    const int m_lane = wm * 128 + r;
+    const unsigned m_lane = (unsigned)(wm * 128 + r);
     auto row_scales = [&](float (&s)[8], const float *of) {
-        int at = m_lane;
-        asm volatile("" : "+v"(at));  // (the places are formed here and not kept in registers over the loop)
+        if constexpr (!EDGE) {
 #pragma unroll
-        for (int i = 0; i < 8; i++) s[i] = of[min(at + 16 * i, last_a)];
+            for (int i = 0; i < 8; i++) s[i] = (of + 16 * i)[m_lane];
+        } else {
+            int at = (int)m_lane;
+            asm volatile("" : "+v"(at));  // (the places are formed here and not kept in registers over the loop)
+#pragma unroll
+            for (int i = 0; i < 8; i++) s[i] = of[min(at + 16 * i, last_a)];
+        }
     };
     const int nblk = min((n0 + wn * 64) / 128, g.wb - 1);
     float sw64 = 0.0f;
@@ -402,10 +411,12 @@ __global__ __launch_bounds__(512, 2) void gemm_block_ring(BlockGemm g, int tiles
 
 int launch_ring(const BlockGemm &g, hipStream_t st) {
     constexpr int LDS = 5 * kRing * 128;
-    if (hipFuncSetAttribute((const void *)gemm_block_ring, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return GR4AD_EHIP;
+    const bool ragged = g.K % 128, edge = g.M % kRing;
+    const auto kernel = ragged ? (edge ? gemm_block_ring<true, true> : gemm_block_ring<true, false>) : (edge ? gemm_block_ring<false, true> : gemm_block_ring<false, false>);
+    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return GR4AD_EHIP;
     const int64_t tiles_m = ceil_div64(g.M, kRing), tiles_n = ceil_div64(g.N, kRing), grid = (tiles_m * tiles_n + 7) / 8 * 8;
     if (grid > 0x3fffffffLL) return GR4AD_EUNSUPPORTED;
-    hipLaunchKernelGGL(gemm_block_ring, dim3((unsigned)grid), dim3(512), LDS, st, g, (int)tiles_m, (int)tiles_n);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(512), LDS, st, g, (int)tiles_m, (int)tiles_n);
     GR4AD_LAUNCH_CHECK();
     return GR4AD_OK;
 }
