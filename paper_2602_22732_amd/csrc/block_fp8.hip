@@ -7,6 +7,8 @@
 //
 // v_mfma_f32_16x16x128_f8f6f4 contracts exactly one block, so a block's product leaves it as 16 x 16 sums that one multiply-add each scales into the
 // float32 accumulators.  The weights are the first operand: a lane then owns one row of A, whose scale is one register, and four consecutive columns of C.
+#include <type_traits>
+
 #include "common.h"
 
 namespace {
@@ -151,42 +153,77 @@ __device__ __forceinline__ void store4(const BlockGemm &g, int m, int n, floatx4
     }
 }
 
-// Up to 16 MG rows: 16 columns of C per workgroup, whose 8 wavefronts take blocks of K in turn and are joined in LDS in their order.
-template <int MG> __global__ __launch_bounds__(512) void gemm_block_few(BlockGemm g) {
+// Up to 16 MG rows: 16 NG columns of C per workgroup, whose 8 wavefronts take blocks of K in turn and are joined in LDS in their order.  (A wavefront reads
+// the rows' fragments anew for every NG column groups: 64 rows x 16384 x 8192 79 us with one group, NG is chosen so that workgroups still fill the chip.)
+template <int MG, int NG> __global__ __launch_bounds__(512) void gemm_block_few(BlockGemm g) {
     constexpr int NW = 8;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, c = lane / 16, n0 = blockIdx.x * 16;
-    const uint8_t *w = g.W + (int64_t)min(n0 + r, g.N - 1) * g.K;
-    const uint8_t *a[MG];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, c = lane / 16, n0 = blockIdx.x * 16 * NG;
+    const uint8_t *w[NG], *a[MG];
     int m[MG];
+#pragma unroll
+    for (int j = 0; j < NG; j++) w[j] = g.W + (int64_t)min(n0 + 16 * j + r, g.N - 1) * g.K;
 #pragma unroll
     for (int i = 0; i < MG; i++) {
         m[i] = min(16 * i + r, g.M - 1);
         a[i] = g.A + (int64_t)m[i] * g.K;
     }
-    floatx4 acc[MG];
+    floatx4 acc[MG][NG];
 #pragma unroll
-    for (int i = 0; i < MG; i++) acc[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int kb = wave; kb < g.nb; kb += NW) {
+    for (int i = 0; i < MG; i++)
+#pragma unroll
+        for (int j = 0; j < NG; j++) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto block = [&](int kb, auto whole) {
         const int k = kb * 128 + 32 * c;
-        const intx8 wf = join8(bytes16(w, k, g.K), bytes16(w, k + 16, g.K));
-        const float sw = g.sw[(int64_t)kb * g.wb + n0 / 128];
+        auto frag = [&](const uint8_t *row) {
+            if constexpr (decltype(whole)::value) {
+                intx8 f;
+                __builtin_memcpy(&f, row + k, 32);
+                return f;
+            } else {
+                return join8(bytes16(row, k, g.K), bytes16(row, k + 16, g.K));
+            }
+        };
+        intx8 wf[NG], af[MG];
+        float s[MG], sw[NG];
+#pragma unroll
+        for (int j = 0; j < NG; j++) {
+            wf[j] = frag(w[j]);
+            sw[j] = g.sw[(int64_t)kb * g.wb + min((n0 + 16 * j) / 128, g.wb - 1)];
+        }
 #pragma unroll
         for (int i = 0; i < MG; i++) {
-            const floatx4 p = mfma_block(wf, join8(bytes16(a[i], k, g.K), bytes16(a[i], k + 16, g.K)));
-            const float s = g.sa[(int64_t)kb * g.M + m[i]] * sw;
-#pragma unroll
-            for (int v = 0; v < 4; v++) acc[i][v] = fmaf(p[v], s, acc[i][v]);
+            af[i] = frag(a[i]);
+            s[i] = g.sa[(int64_t)kb * g.M + m[i]];
         }
-    }
-    __shared__ floatx4 part[NW][MG][64];
 #pragma unroll
-    for (int i = 0; i < MG; i++) part[wave][i][lane] = acc[i];
-    __syncthreads();
-    if (wave < MG) {
-        floatx4 s = part[0][wave][lane];
+        for (int i = 0; i < MG; i++)
 #pragma unroll
-        for (int x = 1; x < NW; x++) s += part[x][wave][lane];
-        store4(g, 16 * wave + r, n0 + 4 * c, s);
+            for (int j = 0; j < NG; j++) {
+                const floatx4 p = mfma_block(wf[j], af[i]);
+#pragma unroll
+                for (int v = 0; v < 4; v++) acc[i][j][v] = fmaf(p[v], s[i] * sw[j], acc[i][j][v]);
+            }
+    };
+    const int whole = g.K / 128;
+    int kb = wave;
+#pragma unroll 2
+    for (; kb < whole; kb += NW) block(kb, std::true_type());
+    if (kb < g.nb) block(kb, std::false_type());  // (the last block, if it is a part of one)
+    constexpr int AT_ONCE = MG * NG < 4 ? MG * NG : 4;  // 16 x 16 tiles that are joined at a time
+    __shared__ floatx4 part[NW][AT_ONCE][64];
+#pragma unroll
+    for (int first = 0; first < MG * NG; first += AT_ONCE) {
+        if (first) __syncthreads();
+#pragma unroll
+        for (int x = 0; x < AT_ONCE; x++) part[wave][x][lane] = acc[(first + x) / NG][(first + x) % NG];
+        __syncthreads();
+        if (wave < AT_ONCE) {
+            const int x = first + wave;
+            floatx4 s = part[0][wave][lane];
+#pragma unroll
+            for (int y = 1; y < NW; y++) s += part[y][wave][lane];
+            store4(g, 16 * (x / NG) + r, n0 + 16 * (x % NG) + 4 * c, s);
+        }
     }
 }
 
@@ -421,6 +458,112 @@ int launch_ring(const BlockGemm &g, hipStream_t st) {
     return GR4AD_OK;
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// Products of a round or two of tiles: TM x TN tiles of C on four wavefronts (2 x 2), operands and row scales straight to LDS, SLOTS blocks of K on their
+// way or in use.  With few tiles the time is one tile's walk along K, so what counts is that a block costs its MFMAs and a barrier and no memory latency.
+// ---------------------------------------------------------------------------------------------------------------------
+template <int TM, int TN, int SLOTS, bool RAGGED> __global__ __launch_bounds__(256) void gemm_block_stream(BlockGemm g) {
+    constexpr int WM = TM / 2, WN = TN / 2, GM = WM / 16, GN = WN / 16, LA = TM / 32, LW = TN / 32, LEAD = SLOTS - 1, LOADS = LA + LW + 1;
+    constexpr int SLOT = (TM + TN) * 128 + 4 * (TM < 64 ? 64 : TM);  // bytes: rows of A, rows of W, A's scales
+    extern __shared__ intx4 smem[];
+    char *lds = (char *)smem;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, c = lane / 16;
+    const int wm = wave / 2, wn = wave % 2, tiles_m = (g.M + TM - 1) / TM;
+    const int m0 = (int)(blockIdx.x % tiles_m) * TM, n0 = (int)(blockIdx.x / tiles_m) * TN;
+    const int last_a = g.M - 1 - m0, last_w = g.N - 1 - n0, ch0 = (lane % 8) ^ ((lane / 8) >> 1);
+    const uint8_t *base_a = g.A + (int64_t)m0 * g.K, *base_w = g.W + (int64_t)n0 * g.K;
+    unsigned a_off[LA], w_off[LW];
+#pragma unroll
+    for (int j = 0; j < LA; j++) a_off[j] = (unsigned)min((wave * LA + j) * 8 + lane / 8, last_a) * (unsigned)g.K + (unsigned)(ch0 ^ (((wave * LA + j) & 1) * 4)) * 16;
+#pragma unroll
+    for (int j = 0; j < LW; j++) w_off[j] = (unsigned)min((wave * LW + j) * 8 + lane / 8, last_w) * (unsigned)g.K + (unsigned)(ch0 ^ (((wave * LW + j) & 1) * 4)) * 16;
+    const int s_row = min((wave * 64) % (TM < 64 ? 64 : TM) + lane, last_a);  // (what several wavefronts load twice is the same)
+    auto dma16 = [&](const void *src, int at) {
+        __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)src, (void __attribute__((address_space(3))) *)(lds + at), 16, 0, 0);
+    };
+    auto dma4 = [&](const void *src, int at) {
+        __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)src, (void __attribute__((address_space(3))) *)(lds + at), 4, 0, 0);
+    };
+    auto issue = [&](int kb, int slot) {
+        const int at = slot * SLOT;
+        auto from = [&](const uint8_t *base, unsigned off, int l) {
+            const uint8_t *src = base + kb * 128 + off;
+            if constexpr (RAGGED)
+                if (kb * 128 + (ch0 ^ ((l & 1) * 4)) * 16 >= g.K) src = zero_chunk;
+            return src;
+        };
+#pragma unroll
+        for (int j = 0; j < LA; j++) dma16(from(base_a, a_off[j], wave * LA + j), at + (wave * LA + j) * 1024);
+#pragma unroll
+        for (int j = 0; j < LW; j++) dma16(from(base_w, w_off[j], wave * LW + j), at + TM * 128 + (wave * LW + j) * 1024);
+        dma4(g.sa + (int64_t)kb * g.M + m0 + s_row, at + (TM + TN) * 128 + (wave * 256) % (4 * (TM < 64 ? 64 : TM)));
+    };
+    typedef const __attribute__((address_space(3))) intx4 *LdsChunk;
+    typedef const __attribute__((address_space(3))) float *LdsFloat;
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)smem, swz = (unsigned)(c ^ ((r >> 1) & 7)) * 16;
+    const unsigned a_lane = lds0 + (unsigned)(wm * WM + r) * 128 + swz, w_lane = lds0 + (unsigned)(TM + wn * WN + r) * 128 + swz, s_lane = lds0 + (unsigned)((TM + TN) * 128 + (wm * WM + r) * 4);
+    auto frag = [&](unsigned at, int i) { return join8(*((LdsChunk)at + i * 128), *((LdsChunk)(at ^ 64u) + i * 128)); };
+    const int nblk = min((n0 + wn * WN) / 128, g.wb - 1);
+    float sw64 = 0.0f;
+    auto weight_scale = [&](int kb) {
+        if (kb % 64 == 0) {
+            const float *src = g.sw + (int64_t)min(kb + lane, g.nb - 1) * g.wb + nblk;
+            asm volatile("global_load_dword %0, %1, off\n\ts_waitcnt vmcnt(0)" : "=&v"(sw64) : "v"(src) : "memory");
+        }
+        return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sw64), kb % 64));
+    };
+    floatx4 acc[GM][GN];
+#pragma unroll
+    for (int i = 0; i < GM; i++)
+#pragma unroll
+        for (int j = 0; j < GN; j++) acc[i][j] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int nb = g.nb;
+#pragma unroll
+    for (int x = 0; x < LEAD; x++) issue(min(x, nb - 1), x);
+    int slot = 0;
+    for (int kb = 0; kb < nb; kb++) {
+        const float sw = weight_scale(kb);
+        // this block has landed, everybody's part of it; the block before is read out, and its slot takes the block LEAD ahead (past the end the last one again,
+        // into slots that nobody reads)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((LEAD - 1) * LOADS) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        issue(min(kb + LEAD, nb - 1), slot == 0 ? LEAD : slot - 1);
+        const unsigned at = (unsigned)slot * SLOT;
+        intx8 wf[GN];
+#pragma unroll
+        for (int j = 0; j < GN; j++) wf[j] = frag(w_lane + at, j);
+#pragma unroll
+        for (int i = 0; i < GM; i++) {
+            const intx8 af = frag(a_lane + at, i);
+            const float s = *((LdsFloat)(s_lane + at) + 16 * i) * sw;
+#pragma unroll
+            for (int j = 0; j < GN; j++) {
+                const floatx4 p = mfma_block(wf[j], af);
+#pragma unroll
+                for (int v = 0; v < 4; v++) acc[i][j][v] = fmaf(p[v], s, acc[i][j][v]);
+            }
+        }
+        slot = slot + 1 == SLOTS ? 0 : slot + 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (loads in flight own their slots)
+#pragma unroll
+    for (int i = 0; i < GM; i++)
+#pragma unroll
+        for (int j = 0; j < GN; j++) store4(g, m0 + wm * WM + 16 * i + r, n0 + wn * WN + 16 * j + 4 * c, acc[i][j]);
+}
+
+template <int TM, int TN, int SLOTS> int launch_stream(const BlockGemm &g, hipStream_t st) {
+    constexpr int LDS = SLOTS * ((TM + TN) * 128 + 4 * (TM < 64 ? 64 : TM));
+    const int64_t grid = ceil_div64(g.M, TM) * ceil_div64(g.N, TN);
+    if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
+    const auto kernel = g.K % 128 ? gemm_block_stream<TM, TN, SLOTS, true> : gemm_block_stream<TM, TN, SLOTS, false>;
+    if (LDS > 65536 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return GR4AD_EHIP;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), LDS, st, g);
+    GR4AD_LAUNCH_CHECK();
+    return GR4AD_OK;
+}
+
 template <int TM, int TN> int launch_tile(const BlockGemm &g, hipStream_t st) {
     const int64_t grid = ceil_div64(g.M, TM) * ceil_div64(g.N, TN);
     if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
@@ -429,18 +572,27 @@ template <int TM, int TN> int launch_tile(const BlockGemm &g, hipStream_t st) {
     return GR4AD_OK;
 }
 
+template <int MG> int launch_few(const BlockGemm &g, hipStream_t st) {
+    // as many column groups per workgroup as leave 256 workgroups
+    const int groups = (g.N + 15) / 16;
+    if (MG > 1 && groups >= 1024) hipLaunchKernelGGL((gemm_block_few<MG, 4>), dim3((groups + 3) / 4), dim3(512), 0, st, g);
+    else if (MG > 1 && groups >= 512) hipLaunchKernelGGL((gemm_block_few<MG, 2>), dim3((groups + 1) / 2), dim3(512), 0, st, g);
+    else hipLaunchKernelGGL((gemm_block_few<MG, 1>), dim3(groups), dim3(512), 0, st, g);
+    GR4AD_LAUNCH_CHECK();
+    return GR4AD_OK;
+}
+
 int launch_block_gemm(const BlockGemm &g, hipStream_t st) {
     ProfScope ps(KC_GEMM_F8_BLOCK, st, 2.0 * (double)g.M * g.N * g.K, ((double)g.M + g.N) * g.K + 2.0 * (double)g.M * g.N);
-    if (g.M <= 64) {
-        const unsigned grid = (unsigned)((g.N + 15) / 16);
-        if (g.M <= 16) hipLaunchKernelGGL(gemm_block_few<1>, dim3(grid), dim3(512), 0, st, g);
-        else if (g.M <= 32) hipLaunchKernelGGL(gemm_block_few<2>, dim3(grid), dim3(512), 0, st, g);
-        else hipLaunchKernelGGL(gemm_block_few<4>, dim3(grid), dim3(512), 0, st, g);
-        GR4AD_LAUNCH_CHECK();
-        return GR4AD_OK;
+    const bool aligned = g.K % 16 == 0 && (uintptr_t)g.A % 16 == 0 && (uintptr_t)g.W % 16 == 0;  // rows in pieces of 16 bytes: direct loads to LDS
+    if (g.M <= 16) return launch_few<1>(g, st);
+    if (g.M <= 32) return launch_few<2>(g, st);
+    if (g.M <= 64) return launch_few<4>(g, st);
+    if (aligned) {
+        if (ceil_div64(g.M, kRing) * ceil_div64(g.N, kRing) >= 192) return launch_ring(g, st);
+        if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) >= 192) return launch_stream<128, 128, 4>(g, st);
+        return launch_stream<64, 64, 4>(g, st);
     }
-    const bool aligned = g.K % 16 == 0 && (uintptr_t)g.A % 16 == 0 && (uintptr_t)g.W % 16 == 0;
-    if (aligned && ceil_div64(g.M, kRing) * ceil_div64(g.N, kRing) >= 192) return launch_ring(g, st);
     if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) < 256) return launch_tile<64, 64>(g, st);
     return launch_tile<128, 128>(g, st);
 }
