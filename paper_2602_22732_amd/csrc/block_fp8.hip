@@ -128,20 +128,24 @@ struct BlockGemm {
     int out_f16;
 };
 
+__device__ __forceinline__ uint16_t half_of(const BlockGemm &g, float x) {
+    uint16_t h;
+    if (g.out_f16) {
+        const _Float16 y = (_Float16)x;
+        __builtin_memcpy(&h, &y, 2);
+    } else {
+        const bf16 y = (bf16)x;
+        __builtin_memcpy(&h, &y, 2);
+    }
+    return h;
+}
 // four consecutive columns of one row of C
 __device__ __forceinline__ void store4(const BlockGemm &g, int m, int n, floatx4 v) {
     if (m >= g.M) return;
     uint16_t h[4];
 #pragma unroll
     for (int e = 0; e < 4; e++) {
-        const float x = v[e] + (g.bias && n + e < g.N ? g.bias[n + e] : 0.0f);
-        if (g.out_f16) {
-            const _Float16 y = (_Float16)x;
-            __builtin_memcpy(&h[e], &y, 2);
-        } else {
-            const bf16 y = (bf16)x;
-            __builtin_memcpy(&h[e], &y, 2);
-        }
+        h[e] = half_of(g, v[e] + (g.bias && n + e < g.N ? g.bias[n + e] : 0.0f));
     }
     uint16_t *dst = (uint16_t *)g.C + (int64_t)m * g.N + n;
     if (n + 4 <= g.N) {
@@ -150,6 +154,41 @@ __device__ __forceinline__ void store4(const BlockGemm &g, int m, int n, floatx4
 #pragma unroll
         for (int e = 0; e < 4; e++)
             if (n + e < g.N) dst[e] = h[e];
+    }
+}
+
+// 16 GM x 16 GN results of a wavefront, through LDS of its own (store_bytes of it) so that they leave as whole rows of 16-byte pieces: pieces of 8 bytes, 32
+// of a row at a time, took a 256 x 256 tile of 16384 x 4096 x 1024 about as long as its products.
+template <int GM, int GN> constexpr int store_bytes() { return 16 * GM * (32 * GN + 16); }
+template <int GM, int GN> __device__ __forceinline__ void store_rows(const BlockGemm &g, char *lds, int m0, int n0, const floatx4 (&acc)[GM][GN]) {
+    const int lane = threadIdx.x % 64, r = lane % 16, c = lane / 16;
+    if (g.N % 8 || (uintptr_t)g.C % 16) {
+#pragma unroll
+        for (int i = 0; i < GM; i++)
+#pragma unroll
+            for (int j = 0; j < GN; j++) store4(g, m0 + 16 * i + r, n0 + 16 * j + 4 * c, acc[i][j]);
+        return;
+    }
+    constexpr int STRIDE = 32 * GN + 16, PER = 2 * GN, ROWS = 64 / PER;  // bytes of a staged row; pieces of a row, rows of one store
+#pragma unroll
+    for (int j = 0; j < GN; j++) {
+        floatx4 b = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (g.bias)
+#pragma unroll
+            for (int e = 0; e < 4; e++) b[e] = g.bias[min(n0 + 16 * j + 4 * c + e, g.N - 1)];
+#pragma unroll
+        for (int i = 0; i < GM; i++) {
+            uint16_t h[4];
+#pragma unroll
+            for (int e = 0; e < 4; e++) h[e] = half_of(g, acc[i][j][e] + b[e]);
+            __builtin_memcpy(lds + (16 * i + r) * STRIDE + (16 * j + 4 * c) * 2, h, 8);
+        }
+    }
+    const int p = lane % PER;
+#pragma unroll 4
+    for (int row = lane / PER; row < 16 * GM; row += ROWS) {
+        const intx4 x = *(const intx4 *)(lds + row * STRIDE + p * 16);
+        if (m0 + row < g.M && n0 + p * 8 < g.N) *(intx4 *)((uint16_t *)g.C + (int64_t)(m0 + row) * g.N + n0 + p * 8) = x;
     }
 }
 
@@ -237,15 +276,22 @@ template <int TM, int TN> __global__ __launch_bounds__(256) void gemm_block_tile
     const int m0 = (int)(blockIdx.x % tiles_m) * TM, n0 = (int)(blockIdx.x / tiles_m) * TN;
     intx4 ra[LA], rw[LW];
     auto load = [&](int kb) {
+        const bool whole = kb * 128 + 128 <= g.K;  // (uniform: only the last block looks at every byte)
+        auto piece = [&](const uint8_t *row, int k) {
+            if (!whole) return bytes16(row, k, g.K);
+            intx4 f;
+            __builtin_memcpy(&f, row + k, 16);
+            return f;
+        };
 #pragma unroll
         for (int i = 0; i < LA; i++) {
             const int id = i * 256 + threadIdx.x;
-            ra[i] = bytes16(g.A + (int64_t)min(m0 + id / 8, g.M - 1) * g.K, kb * 128 + id % 8 * 16, g.K);
+            ra[i] = piece(g.A + (int64_t)min(m0 + id / 8, g.M - 1) * g.K, kb * 128 + id % 8 * 16);
         }
 #pragma unroll
         for (int i = 0; i < LW; i++) {
             const int id = i * 256 + threadIdx.x;
-            rw[i] = bytes16(g.W + (int64_t)min(n0 + id / 8, g.N - 1) * g.K, kb * 128 + id % 8 * 16, g.K);
+            rw[i] = piece(g.W + (int64_t)min(n0 + id / 8, g.N - 1) * g.K, kb * 128 + id % 8 * 16);
         }
     };
     auto slot = [](int row, int p) { return row * 8 + (p ^ ((row >> 1) & 7)); };
@@ -440,10 +486,10 @@ template <bool RAGGED, bool EDGE> __global__ __launch_bounds__(512, 2) void gemm
         a_next = a_free;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (loads in flight own their slots)
-#pragma unroll
-    for (int i = 0; i < 8; i++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) store4(g, m0 + wm * 128 + 16 * i + r, n0 + wn * 64 + 16 * j + 4 * c, acc[i][j]);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    static_assert(8 * store_bytes<8, 4>() <= 5 * HALF * 16, "staged results fit the slots");
+    store_rows<8, 4>(g, (char *)smem + wave * store_bytes<8, 4>(), m0 + wm * 128, n0 + wn * 64, acc);
 }
 
 int launch_ring(const BlockGemm &g, hipStream_t st) {
@@ -547,10 +593,10 @@ template <int TM, int TN, int SLOTS, bool RAGGED> __global__ __launch_bounds__(2
         slot = slot + 1 == SLOTS ? 0 : slot + 1;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (loads in flight own their slots)
-#pragma unroll
-    for (int i = 0; i < GM; i++)
-#pragma unroll
-        for (int j = 0; j < GN; j++) store4(g, m0 + wm * WM + 16 * i + r, n0 + wn * WN + 16 * j + 4 * c, acc[i][j]);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    static_assert(4 * store_bytes<GM, GN>() <= SLOTS * SLOT, "staged results fit the slots");
+    store_rows<GM, GN>(g, lds + wave * store_bytes<GM, GN>(), m0 + wm * WM, n0 + wn * WN, acc);
 }
 
 template <int TM, int TN, int SLOTS> int launch_stream(const BlockGemm &g, hipStream_t st) {
@@ -590,7 +636,7 @@ int launch_block_gemm(const BlockGemm &g, hipStream_t st) {
     if (g.M <= 64) return launch_few<4>(g, st);
     if (aligned) {
         if (ceil_div64(g.M, kRing) * ceil_div64(g.N, kRing) >= 192) return launch_ring(g, st);
-        if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) >= 192) return launch_stream<128, 128, 4>(g, st);
+        if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) >= 192) return launch_stream<128, 128, 2>(g, st);
         return launch_stream<64, 64, 4>(g, st);
     }
     if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) < 256) return launch_tile<64, 64>(g, st);
