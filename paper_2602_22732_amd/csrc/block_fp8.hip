@@ -40,12 +40,13 @@ struct BlockScale {
     }
 };
 
-// Sixteen lanes hold a row's block, eight values each.  TALL: a workgroup owns one block of 128 x 128 (16 rows at a time, 8 times); otherwise 16 rows
+// Sixteen lanes hold a row's block, eight values each.  wide: workgroups along a row, which are successive ones (bf16, 16384 x 4096: 50 us; with the rows in
+// turn 55).  keep: the bytes stay in the caches; outputs that would fill them and lie on 8 bytes pass by (44 us).  TALL: a workgroup owns one block of 128 x 128 (16 rows at a time, 8 times); otherwise 16 rows
 // by STEPS blocks, all of whose values are requested at once.
 template <typename T, bool TALL> __global__ __launch_bounds__(256) void quantize_blocks(const T *__restrict__ x, int64_t ldx, uint8_t *__restrict__ q, float *__restrict__ scale, int rows,
-                                                                                        int n, int nb, int bands) {
-    constexpr int STEPS = TALL ? 8 : sizeof(T) == 2 ? 4 : 2;
-    const int band = blockIdx.x % bands, kb0 = blockIdx.x / bands * (TALL ? 1 : STEPS), lane16 = threadIdx.x % 16, r16 = threadIdx.x / 16;
+                                                                                        int n, int wide, int bands, int keep) {
+    constexpr int STEPS = TALL ? 8 : 2;
+    const int band = blockIdx.x / wide, kb0 = blockIdx.x % wide * (TALL ? 1 : STEPS), lane16 = threadIdx.x % 16, r16 = threadIdx.x / 16;
     float v[STEPS][8], amax[STEPS];
     auto row_of = [&](int i) { return TALL ? band * 128 + i * 16 + r16 : band * 16 + r16; };
     auto col_of = [&](int i) { return (TALL ? kb0 : kb0 + i) * 128 + lane16 * 8; };
@@ -96,7 +97,8 @@ template <typename T, bool TALL> __global__ __launch_bounds__(256) void quantize
         const uint2 w = e4m3x8(v[i], s.inv);
         uint8_t *dst = q + (int64_t)r * n + c;
         if (c + 8 <= n) {
-            __builtin_memcpy(dst, &w, 8);
+            if (keep) __builtin_memcpy(dst, &w, 8);
+            else __builtin_nontemporal_store((uint64_t)w.y << 32 | w.x, (uint64_t *)dst);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; e++)
@@ -655,11 +657,12 @@ int gr4ad_op_quantize_blocks(gr4ad_dtype dtype, const void *x, int64_t x_stride,
     const size_t e = dtype == GR4AD_BF16 ? 2 : 4;
     if ((uintptr_t)x % e || (uintptr_t)scale % 4) return gr4ad_set_thread_error(GR4AD_EINVAL, "quantize_blocks: misaligned pointer");
     const bool tall = block_rows == 128;
-    const int64_t nb = ceil_div64(n, 128), bands = ceil_div64(rows, tall ? 128 : 16), steps = tall ? 1 : e == 2 ? 4 : 2, grid = bands * ceil_div64(nb, steps);
+    const int64_t nb = ceil_div64(n, 128), bands = ceil_div64(rows, tall ? 128 : 16), steps = tall ? 1 : 2, wide = ceil_div64(nb, steps), grid = bands * wide;
+    const int keep = (int64_t)rows * n < (8 << 20) || n % 8 || (uintptr_t)q % 8;
     if (grid > 0x7fffffffLL) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "quantize_blocks: %d rows of %d values", rows, n);
     hipStream_t st = (hipStream_t)hip_stream;
     ProfScope ps(KC_QUANTIZE_BLOCKS, st, 0.0, (double)rows * n * (e + 1));
-#define QUANTIZE_(T, TALL) hipLaunchKernelGGL((quantize_blocks<T, TALL>), dim3((unsigned)grid), dim3(256), 0, st, (const T *)x, x_stride, (uint8_t *)q, scale, rows, n, (int)nb, (int)bands)
+#define QUANTIZE_(T, TALL) hipLaunchKernelGGL((quantize_blocks<T, TALL>), dim3((unsigned)grid), dim3(256), 0, st, (const T *)x, x_stride, (uint8_t *)q, scale, rows, n, (int)wide, (int)bands, keep)
     if (dtype == GR4AD_BF16) { if (tall) QUANTIZE_(bf16, true); else QUANTIZE_(bf16, false); }
     else if (tall) QUANTIZE_(float, true);
     else QUANTIZE_(float, false);
