@@ -288,14 +288,16 @@ int gr4ad_op_gather_rows(gr4ad_dtype dtype, const void *src_dev, const int32_t *
  *                  A page number outside [0, n_pages): the positions on it count as absent.
  *   q              [N, H, dh] dtype, rows q_stride elements apart (a part of a wider row is fine)
  *   k_new, v_new   [N, H_kv, dh] dtype, rows kv_stride elements apart: written into their pages first; both NULL if the pages hold them already.
- *                  No two new tokens may lie on one slot of one page
+ *                  No two new tokens may lie on one slot of one page, and a page that receives new tokens stands at one place of one sequence's
+ *                  table (pages that a call only reads may stand anywhere)
  *   q_start        [B+1] int32 device, ascending from >= 0 to <= N; rows in no sequence are left as they are.  seq_len [B] int32 device, at most
  *                  max_pages * page_size (clamped).  Tokens at negative positions (seq_len[b] < m_b) are neither written nor see anything
  *   out            [N, H, dh] dtype, dense
  *   workspace_dev  gr4ad_op_paged_attention_workspace_bytes bytes of scratch (0: none), not shared by calls that overlap in time
- * float32 sums, maxima and normalisers; bf16 weights of the softmax are rounded once, as operands of the product with the values.  Same bits from run
- * to run; a row's bits may depend on the batch it is in (which decides how its keys are split).  head widths 16, 32, 64, 128; page_size a power of two
- * from 16 to 1024; q, k_new and v_new with their rows, out, both page arrays and the workspace 16-byte aligned.
+ * float32 sums, maxima and normalisers; in bf16, long chunks round the softmax's weights once, as operands of the product with the values, and other
+ * rows enter them as two bf16 numbers.  Same bits from run to run; a row's bits may depend on the batch it is in (which decides how its keys are split).
+ * B, N >= 1; head widths 16, 32, 64, 128; page_size a power of two from 16 to 1024; q, k_new and v_new with their rows, out, both page arrays and the
+ * workspace 16-byte aligned.
  */
 typedef struct {
     void *k_pages, *v_pages;         /* device, of the call's dtype */
@@ -314,7 +316,7 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
  *   scale = amax / 448 and q = nearest OCP E4M3 value (ties to even) of x * (448 / amax), amax the block's largest magnitude (float32 operations);
  *   a block with amax < 2^-100 becomes zeros with scale 1.  A NaN becomes the E4M3 NaN; of a block that holds an infinity nothing is defined but that it has NaNs.
  * x [rows, n] float32 or bf16, rows x_stride elements apart; q [rows, n] bytes; scale [ceil(n / 128), ceil(rows / block_rows)] float32: blocks along n
- * first, as the product reads them.  Any rows and n >= 1; the last blocks may be partial.
+ * first, as the product reads them.  Any rows and n from 1 to 2^31 - 256; the last blocks may be partial.
  */
 int gr4ad_op_quantize_blocks(gr4ad_dtype dtype, const void *x_dev, int64_t x_stride, void *q_dev, float *scale_dev, int32_t rows, int32_t n, int32_t block_rows,
                              void *hip_stream);
@@ -324,7 +326,7 @@ int gr4ad_op_quantize_blocks(gr4ad_dtype dtype, const void *x_dev, int64_t x_str
  * on operands of gr4ad_op_quantize_blocks (Aq with block_rows = 1, Wq with block_rows = 128): a_scale [ceil(K/128), M], w_scale [ceil(K/128), ceil(N/128)],
  * bias [N] float32 or NULL.  Every block's product is scaled and added in float32.  C is bf16, or IEEE half with out_f16 != 0 (logits for
  * gr4ad_op_adjust_logits_f16 and gr4ad_op_select_f16): the matrix cores keep about 16 bits of an FP8 product's sum, so there is no float32 form.
- * Any M, N, K >= 1; rows dense.
+ * Any M, N, K from 1 to 2^31 - 256; rows dense.
  */
 int gr4ad_op_linear_fp8_block(const void *Aq_dev, const float *a_scale_dev, const void *Wq_dev, const float *w_scale_dev, const float *bias_dev, void *C_dev,
                               int32_t M, int32_t N, int32_t K, int32_t out_f16, void *hip_stream);
@@ -334,8 +336,8 @@ int gr4ad_op_linear_fp8_block(const void *Aq_dev, const float *a_scale_dev, cons
  * times token v occurs in the row's history, in float32 and in this order:
  *   l = c > 0 ? (l > 0 ? l / repetition : l * repetition) : l;   l -= frequency * c + (c > 0 ? presence : 0);   l += bias[bias_row, v];
  *   l = -inf where the row's mask forbids v (whatever the logit holds).
- * logits, out [rows, V] float32 (_f16: IEEE half, rounded once), out may be logits itself.  Every rule is optional (NULL).  The struct is host memory,
- * its pointers device memory.
+ * logits, out [rows, V] float32 (_f16: IEEE half, rounded once), out may be logits itself.  rows >= 1, V from 1 to 2^30.  Every rule is optional (NULL).
+ * The struct is host memory, its pointers device memory.
  */
 typedef struct {
     const int32_t *history;      /* [rows, history_stride]: earlier tokens of each row, any order; entries outside [0, V) are passed over */

@@ -494,13 +494,15 @@ template <bool RAGGED, bool EDGE> __global__ __launch_bounds__(512, 2) void gemm
     store_rows<8, 4>(g, (char *)smem + wave * store_bytes<8, 4>(), m0 + wm * 128, n0 + wn * 64, acc);
 }
 
+int too_many_tiles(const BlockGemm &g) { return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "linear_fp8_block: sizes %d x %d x %d", g.M, g.N, g.K); }
+
 int launch_ring(const BlockGemm &g, hipStream_t st) {
     constexpr int LDS = 5 * kRing * 128;
     const bool ragged = g.K % 128, edge = g.M % kRing;
     const auto kernel = ragged ? (edge ? gemm_block_ring<true, true> : gemm_block_ring<true, false>) : (edge ? gemm_block_ring<false, true> : gemm_block_ring<false, false>);
-    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return GR4AD_EHIP;
     const int64_t tiles_m = ceil_div64(g.M, kRing), tiles_n = ceil_div64(g.N, kRing), grid = (tiles_m * tiles_n + 7) / 8 * 8;
-    if (grid > 0x3fffffffLL) return GR4AD_EUNSUPPORTED;
+    if (grid > 0x3fffffffLL) return too_many_tiles(g);
+    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return GR4AD_EHIP;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(512), LDS, st, g, (int)tiles_m, (int)tiles_n);
     GR4AD_LAUNCH_CHECK();
     return GR4AD_OK;
@@ -604,7 +606,7 @@ template <int TM, int TN, int SLOTS, bool RAGGED> __global__ __launch_bounds__(2
 template <int TM, int TN, int SLOTS> int launch_stream(const BlockGemm &g, hipStream_t st) {
     constexpr int LDS = SLOTS * ((TM + TN) * 128 + 4 * (TM < 64 ? 64 : TM));
     const int64_t grid = ceil_div64(g.M, TM) * ceil_div64(g.N, TN);
-    if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
+    if (grid > 0x7fffffffLL) return too_many_tiles(g);
     const auto kernel = g.K % 128 ? gemm_block_stream<TM, TN, SLOTS, true> : gemm_block_stream<TM, TN, SLOTS, false>;
     if (LDS > 65536 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return GR4AD_EHIP;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), LDS, st, g);
@@ -614,7 +616,7 @@ template <int TM, int TN, int SLOTS> int launch_stream(const BlockGemm &g, hipSt
 
 template <int TM, int TN> int launch_tile(const BlockGemm &g, hipStream_t st) {
     const int64_t grid = ceil_div64(g.M, TM) * ceil_div64(g.N, TN);
-    if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
+    if (grid > 0x7fffffffLL) return too_many_tiles(g);
     hipLaunchKernelGGL((gemm_block_tile<TM, TN>), dim3((unsigned)grid), dim3(256), 0, st, g);
     GR4AD_LAUNCH_CHECK();
     return GR4AD_OK;
@@ -632,7 +634,8 @@ template <int MG> int launch_few(const BlockGemm &g, hipStream_t st) {
 
 int launch_block_gemm(const BlockGemm &g, hipStream_t st) {
     ProfScope ps(KC_GEMM_F8_BLOCK, st, 2.0 * (double)g.M * g.N * g.K, ((double)g.M + g.N) * g.K + 2.0 * (double)g.M * g.N);
-    const bool aligned = g.K % 16 == 0 && (uintptr_t)g.A % 16 == 0 && (uintptr_t)g.W % 16 == 0;  // rows in pieces of 16 bytes: direct loads to LDS
+    // rows in pieces of 16 bytes (and a tile's rows within 32 bits of its first): direct loads to LDS
+    const bool aligned = g.K % 16 == 0 && g.K < (1 << 23) && (uintptr_t)g.A % 16 == 0 && (uintptr_t)g.W % 16 == 0;
     if (g.M <= 16) return launch_few<1>(g, st);
     if (g.M <= 32) return launch_few<2>(g, st);
     if (g.M <= 64) return launch_few<4>(g, st);
@@ -659,7 +662,7 @@ int gr4ad_op_quantize_blocks(gr4ad_dtype dtype, const void *x, int64_t x_stride,
     const bool tall = block_rows == 128;
     const int64_t nb = ceil_div64(n, 128), bands = ceil_div64(rows, tall ? 128 : 16), steps = tall ? 1 : 2, wide = ceil_div64(nb, steps), grid = bands * wide;
     const int keep = (int64_t)rows * n < (8 << 20) || n % 8 || (uintptr_t)q % 8;
-    if (grid > 0x7fffffffLL) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "quantize_blocks: %d rows of %d values", rows, n);
+    if (grid > 0x7fffffffLL || n > 0x7fffff00) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "quantize_blocks: %d rows of %d values", rows, n);
     hipStream_t st = (hipStream_t)hip_stream;
     ProfScope ps(KC_QUANTIZE_BLOCKS, st, 0.0, (double)rows * n * (e + 1));
 #define QUANTIZE_(T, TALL) hipLaunchKernelGGL((quantize_blocks<T, TALL>), dim3((unsigned)grid), dim3(256), 0, st, (const T *)x, x_stride, (uint8_t *)q, scale, rows, n, (int)wide, (int)bands, keep)

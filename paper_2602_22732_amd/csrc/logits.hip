@@ -129,7 +129,7 @@ template <typename T> int adjust(const T *in, T *out, int32_t rows, int32_t V, c
     constexpr int E = Piece<T>::N;
     const int each = one ? E : 2 * E, threads = V <= 64 * each ? 64 : V <= 128 * each ? 128 : 256, span = threads * each;
     const int64_t stretches = ceil_div64(V, span), grid = rows * stretches;
-    if (grid > 0x7fffffffLL) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "adjust_logits: %d rows of %d logits", rows, V);
+    if (grid > 0x7fffffffLL || V > (1 << 30)) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "adjust_logits: %d rows of %d logits", rows, V);
     const int keep = (int64_t)rows * V * (int)sizeof(T) < (16 << 20) || V * sizeof(T) % 16 || (uintptr_t)out % 16;
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(KC_ADJUST_LOGITS, st, 0.0, 2.0 * sizeof(T) * rows * (double)V);

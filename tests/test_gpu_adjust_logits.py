@@ -117,6 +117,18 @@ def test_writes_nothing_outside(dtype):
         assert go.intact()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_large_outputs_are_those_of_their_parts(dtype):
+    # beyond the sizes from which results pass the caches and a thread takes two pieces
+    g = torch.Generator().manual_seed(8)
+    rows, V = 2100, 4104
+    x, r = torch.randn(rows, V, generator=g).to(dtype).cuda(), {k: v.cuda() for k, v in rules(g, rows, V, ("history", "bias", "mask")).items()}
+    got = binding.op_adjust_logits(x, **r)
+    for a, b in ((0, 700), (700, 2100)):
+        part = {k: v if k in ("bias", "mask") else v[a:b] for k, v in r.items()}
+        assert torch.equal(got[a:b], binding.op_adjust_logits(x[a:b], **part))
+
+
 def test_a_step_through_the_operators():
     """Attention over pages -> projection and classifier on FP8 blocks -> masks and penalties -> selection, captured and replayed: the selection keeps only
     allowed tokens and agrees with the definition on the logits it was given, and every replay with eager calls."""

@@ -135,8 +135,9 @@ def test_product_writes_nothing_outside():
         assert (gc.typed(torch.bfloat16, (M, N)) == float(K)).all()   # K < 2^8 or K = 256: exact in bf16
 
 
-def test_captured_product_and_quantiser():
-    x, w = torch.randn(70, 640, device="cuda").bfloat16(), torch.randn(300, 640, device="cuda").bfloat16()
+@pytest.mark.parametrize("M,N", [(70, 300), (9, 300), (1100, 4100), (4100, 3100)])
+def test_captured_product_and_quantiser(M, N):
+    x, w = torch.randn(M, 640, device="cuda").bfloat16(), torch.randn(N, 640, device="cuda").bfloat16()
     wq, sw = binding.op_quantize_blocks(w, 128)
 
     def step():
@@ -149,7 +150,7 @@ def test_captured_product_and_quantiser():
     with torch.cuda.graph(graph):
         out = step()
     for seed in range(4):
-        x.copy_(torch.randn(70, 640, generator=torch.Generator().manual_seed(seed)))
+        x.copy_(torch.randn(M, 640, generator=torch.Generator().manual_seed(seed)))
         torch.cuda.synchronize()
         graph.replay()
         torch.cuda.synchronize()
@@ -166,3 +167,38 @@ def test_results_repeat_to_the_bit():
         runs.append((q, s, binding.op_linear_fp8_block(q, s, wq, sw, out_dtype=torch.float16)))
     assert all(torch.equal(a, b) for a, b in zip(*runs))
     np.testing.assert_array_equal(runs[0][2].cpu().numpy(), runs[1][2].cpu().numpy())
+
+
+def test_rows_of_many_millions_of_values():
+    M, N, K = 70, 3, 1 << 24
+    A, W = torch.zeros(M, K, dtype=torch.uint8, device="cuda"), torch.zeros(N, K, dtype=torch.uint8, device="cuda")
+    A[:, -300:] = 0x38                                          # 1.0
+    A[66, 5] = 0x40                                             # 2.0
+    W[1, :] = 0x38
+    sa = torch.ones(K // 128, M, device="cuda")
+    sa[-1] = torch.arange(M, device="cuda").float()
+    out = binding.op_linear_fp8_block(A, sa, W, torch.ones(K // 128, 1, device="cuda"), out_dtype=torch.float16).float().cpu()
+    want = torch.zeros(M, N)
+    want[:, 1] = 172 + 128 * torch.arange(M).float()
+    want[66, 1] += 2
+    assert torch.equal(out, want.half().float())
+
+
+@pytest.mark.parametrize("M,N,K", [(70, 300, 640), (1100, 4104, 256), (4100, 3104, 256), (5, 40, 256)])
+def test_results_at_an_odd_place(M, N, K):
+    x, w = torch.randn(M, K, device="cuda").bfloat16(), torch.randn(N, K, device="cuda").bfloat16()
+    operands = (*binding.op_quantize_blocks(x), *binding.op_quantize_blocks(w, 128))
+    want = binding.op_linear_fp8_block(*operands)
+    room = torch.zeros(M * N + 8, device="cuda", dtype=torch.bfloat16)
+    got = binding.op_linear_fp8_block(*operands, out=room[3:3 + M * N].view(M, N))
+    assert torch.equal(got, want) and not room[:3].any() and not room[3 + M * N:].any()
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_large_quantised_outputs(block_rows):
+    # beyond the size from which results pass the caches: the same as in parts
+    x = torch.randn(2050, 4168, device="cuda").bfloat16()
+    q, scale = binding.op_quantize_blocks(x, block_rows)
+    for a, b in ((0, 1024), (1024, 2050)):
+        qp, sp = binding.op_quantize_blocks(x[a:b], block_rows)
+        assert torch.equal(q[a:b], qp) and torch.equal(scale[:, a // block_rows:-(-b // block_rows)], sp)

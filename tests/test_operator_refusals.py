@@ -46,6 +46,7 @@ def test_attention_workspace():
 @pytest.mark.parametrize("args,status", [
     ((0, None, 8, P, P, 1, 8, 1), -1), ((0, P, 8, None, P, 1, 8, 1), -1), ((0, P, 8, P, None, 1, 8, 1), -1), ((3, P, 8, P, P, 1, 8, 1), -1), ((0, P, 8, P, P, 0, 8, 1), -1),
     ((0, P, 7, P, P, 1, 8, 1), -1), ((0, P, 8, P, P, 1, 8, 64), -2), ((0, P + 2, 8, P, P, 1, 8, 1), -1), ((0, P, 8, P, P + 1, 1, 8, 1), -1), ((0, P, 2 ** 31 - 1, P, P, 2 ** 31 - 1, 2 ** 31 - 1, 1), -2),
+    ((0, P, 2 ** 31 - 1, P, P, 1, 2 ** 31 - 1, 1), -2),
 ])
 def test_quantize_refuses(args, status):
     assert binding.lib().gr4ad_op_quantize_blocks(*args, None) == status
@@ -56,6 +57,7 @@ def test_quantize_refuses(args, status):
     ((None, P, P, P, None, P, 1, 1, 1, 0), -1), ((P, None, P, P, None, P, 1, 1, 1, 0), -1), ((P, P, None, P, None, P, 1, 1, 1, 0), -1), ((P, P, P, None, None, P, 1, 1, 1, 0), -1),
     ((P, P, P, P, None, None, 1, 1, 1, 0), -1), ((P, P, P, P, None, P, 0, 1, 1, 0), -1), ((P, P, P, P, None, P, 1, 0, 1, 0), -1), ((P, P, P, P, None, P, 1, 1, 0, 0), -1),
     ((P, P, P, P, None, P + 1, 1, 1, 1, 0), -1), ((P, P + 2, P, P, None, P, 1, 1, 1, 0), -1), ((P, P, P, P, P + 2, P, 1, 1, 1, 0), -1), ((P, P, P, P, None, P, 2 ** 31 - 1, 1, 1, 0), -2),
+    ((P, P, P, P, None, P, 2 ** 31 - 300, 2 ** 31 - 300, 128, 0), -2), ((P, P, P, P, None, P, 2 ** 31 - 300, 2 ** 31 - 300, 130, 0), -2),
 ])
 def test_linear_refuses(args, status):
     assert binding.lib().gr4ad_op_linear_fp8_block(*args, None) == status
@@ -74,6 +76,8 @@ def test_adjust_refuses(over, rows, V, needle):
         assert entry(None, P, 1, 8, C.byref(binding.LogitRules()), None) == -1
         assert entry(P, P + 1, 1, 8, C.byref(binding.LogitRules()), None) == -1
         assert entry(P, P, 1, 8, None, None) == -1
+        for size in ((1, 2 ** 30 + 1), (2 ** 31 - 1, 2 ** 30)):
+            assert entry(P, P, *size, C.byref(binding.LogitRules()), None) == -2
 
 
 def test_binding_refuses_tensors_that_are_not_on_a_gpu():
