@@ -1135,20 +1135,20 @@ Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, 
     // Workgroups enough to fill the chip (counted as if all sequences had the same number of rows): one per compute unit for tiles of 256 rows, two for the
     // others (tiles of 32 rows, 840 of them: 130 us alone, 136 in halves with their join); with tiles of 16 rows, which stand for many sequences of their
     // own lengths, four where that many are near (512 of up to 8192 keys: alone 261 us, in halves 233, in quarters 238; 16 of 100000 keys in 16 parts 175 us, in
-    // 64 parts 189).  A part has 256 (1024) keys at least.
+    // 64 parts 189).  A part has 256 keys at least (1024 of the staged kinds), and a tile of 16 rows with 256 KB of keys and values at most stays whole: the parts would wait
+    // longer for their join than they save (one row of 777 keys, calls in a row: bf16 of 64 columns 9.8 us against 14.7; fp32 of 128, twice beyond: 23.4 against 15.2).
     const int64_t blocks = (int64_t)B * ceil_div64(rows, p.rows) * Hkv, enough = p.rows == kFlashRows ? 256 : p.rows == 16 && blocks >= 256 ? 1024 : 512, least = flash ? 1024 : 256;
     int64_t keys = (int64_t)max_pages * page;
     if (window && (int64_t)window + sinks + 64 < keys) keys = (int64_t)window + sinks + 64;
     const int64_t want = (enough + blocks - 1) / blocks, most = (keys + least - 1) / least, n = want < most ? want : most;
-    p.nsplit = (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+    const bool whole = p.rows == 16 && keys * 2 * dh * (dtype == GR4AD_BF16 ? 2 : 4) <= 256 << 10;
+    p.nsplit = (int)(whole || n < 1 ? 1 : n > 64 ? 64 : n);
     p.bytes = p.nsplit > 1 ? (size_t)N * H * p.nsplit * (dh + 2) * sizeof(float) : 0;
     return p;
 }
 
-// More than 64 KB of LDS has to be asked for, once per kernel and device.
+// More than 64 KB of LDS has to be asked for, on each device: every launch asks for its own.
 int allow_lds(const void *kernel, int bytes) {
-    int device = 0;
-    if (hipGetDevice(&device) != hipSuccess || device < 0) return GR4AD_EHIP;
     return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess ? GR4AD_OK : GR4AD_EHIP;
 }
 

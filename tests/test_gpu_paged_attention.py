@@ -271,3 +271,70 @@ def test_two_graphs_that_share_a_workspace_and_another_stream():
             again = binding.op_paged_attention(*args, **new)
             torch.cuda.synchronize()
             assert same(again, eager)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_more_sequences_than_a_wavefront_counts_at_once(dtype):
+    new = [1] * 70 + [0, 5] + [1] * 60 + [33]
+    check(Case(dtype, 64, 4, 1, 16, new=new, lens=[max(m, 1 + 7 * i % 90) for i, m in enumerate(new)], seed=16))
+
+
+@pytest.mark.parametrize("dh,H,H_kv,page", [(32, 4, 2, 16), (64, 8, 2, 64), (128, 8, 2, 32), (128, 16, 2, 128)])
+def test_long_chunks(dh, H, H_kv, page):
+    # tiles of 256 rows, of 128, several of them, under a window and without
+    for new, lens in (([300, 40], [1000, 41]), ([100], [700])):
+        c = Case("bf16", dh, H, H_kv, page, new, lens, seed=dh + H)
+        check(c)
+        check(c, window=150, sinks=9)
+
+
+def test_a_captured_long_chunk_and_values_that_are_no_numbers_in_it():
+    c = Case("bf16", 128, 16, 2, 64, new=[300], lens=[900], seed=17)
+    c.v_new[250] = float("inf")
+    want, tol = c.expected()
+    args = [t.cuda() for t in (c.q, c.k, c.v, c.table, torch.tensor(c.starts, dtype=torch.int32), torch.tensor(c.lens, dtype=torch.int32))]
+    new = dict(k_new=c.k_new.cuda(), v_new=c.v_new.cuda())
+    eager = binding.op_paged_attention(*args, **new)
+    torch.cuda.synchronize()
+    assert ((eager.cpu().double()[:250] - want[:250]).abs() <= tol[:250]).all()
+    assert (eager[250:] == float("inf")).all()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = binding.op_paged_attention(*args, **new)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(out, eager)
+
+
+@pytest.mark.parametrize("dtype,dh,H,H_kv,page", [("bf16", 64, 4, 1, 64), ("bf16", 128, 8, 1, 16), ("bf16", 16, 2, 2, 256), ("f32", 128, 2, 1, 32), ("f32", 32, 4, 2, 1024), ("f32", 16, 3, 1, 64)])
+def test_keys_shared_by_workgroups(dtype, dh, H, H_kv, page):
+    # up to 20 stretches of keys for a tile, most of which short sequences leave empty
+    c = Case(dtype, dh, H, H_kv, page, new=[1, 2, 1, 0, 3], lens=[5000, 2, 1300, 900, 2600], seed=dh)
+    check(c)
+    check(c, window=2000, sinks=3)
+
+
+def test_a_long_chunk_whose_keys_workgroups_share():
+    c = Case("bf16", 64, 2, 1, 64, new=[70, 0, 9], lens=[6000, 40, 2100], seed=18)
+    c.table[0, 20], c.table[2, 3] = -1, c.n_pages
+    check(c)
+    check(c, window=1500, sinks=100)
+
+
+def test_two_streams_at_once():
+    cases = [Case("bf16", 64, 4, 1, 64, new=[1, 1, 20], lens=[3000, 40, 400], seed=19), Case("f32", 32, 4, 2, 16, new=[2, 1], lens=[100, 2500], seed=20)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    on_gpu = [[t.cuda() for t in (c.q, c.k, c.v, c.table, torch.tensor(c.starts, dtype=torch.int32), torch.tensor(c.lens, dtype=torch.int32), c.k_new, c.v_new)] for c in cases]
+    torch.cuda.synchronize()
+    outs = [[] for _ in cases]
+    for _ in range(4):
+        for i, args in enumerate(on_gpu):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(binding.op_paged_attention(*args))
+    torch.cuda.synchronize()
+    for c, got in zip(cases, outs):
+        want, tol = c.expected()
+        assert all(same(g, got[0]) for g in got)
+        assert ((got[0].cpu().double() - want).abs() <= tol).all()
