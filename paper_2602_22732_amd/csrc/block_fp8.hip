@@ -1,9 +1,11 @@
 // FP8 (OCP E4M3) operands with a scale for every block of 128 values along the contraction, and their product:
 //     C[m, n] = sum_kb sa[kb, m] sw[kb, n / 128] sum_{k in block kb} Aq[m, k] Wq[n, k]  (+ bias[n]).
 //
-//  * quantize_blocks<..>   1 x 128 or 128 x 128 blocks, one pass over the values.
-//  * gemm_block_few<MG>    up to 64 rows: the weights stream from memory to the matrix cores' operands, wavefronts split K.
-//  * gemm_block_tile<..>   tiles of C, operands staged in LDS.
+//  * quantize_blocks<..>     1 x 128 or 128 x 128 blocks, one pass over the values.
+//  * gemm_block_few<..>      up to 64 rows: the weights stream from memory to the matrix cores' operands, wavefronts split K.
+//  * gemm_block_ring<..>     256 x 256 tiles of C, for products that have enough of them to fill the chip.
+//  * gemm_block_stream<..>   128 x 128 and 64 x 64 tiles for the shapes between.
+//  * gemm_block_tile<..>     the same tiles for rows that do not start on 16 bytes.
 //
 // v_mfma_f32_16x16x128_f8f6f4 contracts exactly one block, so a block's product leaves it as 16 x 16 sums that one multiply-add each scales into the
 // float32 accumulators.  The weights are the first operand: a lane then owns one row of A, whose scale is one register, and four consecutive columns of C.
@@ -40,9 +42,11 @@ struct BlockScale {
     }
 };
 
-// Sixteen lanes hold a row's block, eight values each.  wide: workgroups along a row, which are successive ones (bf16, 16384 x 4096: 50 us; with the rows in
-// turn 55).  keep: the bytes stay in the caches; outputs that would fill them and lie on 8 bytes pass by (44 us).  TALL: a workgroup owns one block of 128 x 128 (16 rows at a time, 8 times); otherwise 16 rows
-// by STEPS blocks, all of whose values are requested at once.
+// Sixteen lanes hold a row's block, eight values each.  TALL: a workgroup owns one block of 128 x 128 (16 rows at a time, 8 times); otherwise 16 rows by STEPS
+// blocks.  All of a thread's values are requested at once and kept, so they are read once.  wide: workgroups along a row, which are successive ones (bf16,
+// 16384 x 4096: 50 us; with the rows in turn 55).  keep: the bytes stay in the caches; outputs that would fill them and lie on 8 bytes pass by (41 us).
+// Bound by the bytes: bf16, 4096 x 4096 in rows 12 us, 4.2 TB/s; float32, 16384 x 1040 in squares 18 us, 4.7 TB/s, 16384 x 4096 50 us, 6.7 TB/s (with
+// outputs that stay in the caches 59).
 template <typename T, bool TALL> __global__ __launch_bounds__(256) void quantize_blocks(const T *__restrict__ x, int64_t ldx, uint8_t *__restrict__ q, float *__restrict__ scale, int rows,
                                                                                         int n, int wide, int bands, int keep) {
     constexpr int STEPS = TALL ? 8 : 2;
@@ -195,7 +199,8 @@ template <int GM, int GN> __device__ __forceinline__ void store_rows(const Block
 }
 
 // Up to 16 MG rows: 16 NG columns of C per workgroup, whose 8 wavefronts take blocks of K in turn and are joined in LDS in their order.  (A wavefront reads
-// the rows' fragments anew for every NG column groups: 64 rows x 16384 x 8192 79 us with one group, NG is chosen so that workgroups still fill the chip.)
+// the rows' fragments anew for every NG column groups: 64 rows x 16384 x 8192 79 us with one group, 38 with four, 3.5 TB/s; NG is chosen so that workgroups
+// still fill the chip.)  Few and small ones are latency: 5 x 4096 x 1024 3.4 us, where the weights' bytes are worth 0.8.
 template <int MG, int NG> __global__ __launch_bounds__(512) void gemm_block_few(BlockGemm g) {
     constexpr int NW = 8;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, c = lane / 16, n0 = blockIdx.x * 16 * NG;
@@ -268,8 +273,9 @@ template <int MG, int NG> __global__ __launch_bounds__(512) void gemm_block_few(
     }
 }
 
-// TM x TN tiles of C on four wavefronts (2 x 2).  The next block's operands travel to registers while this one's multiply.  A tile row is one block, 128
-// bytes; its 16-byte chunk p lies at p ^ (row / 2 % 8).
+// Rows that do not start on 16 bytes, or are too long for 32-bit places: TM x TN tiles of C on four wavefronts (2 x 2).  The next block's operands travel to
+// registers while this one's multiply.  A tile row is one block, 128 bytes; its 16-byte chunk p lies at p ^ (row / 2 % 8).  3000 x 5000 x 1111: 57 us,
+// 0.58 PFLOP/s; 200 x 300 x 1999 17 us, the walk of one tile along K.
 template <int TM, int TN> __global__ __launch_bounds__(256) void gemm_block_tile(BlockGemm g) {
     constexpr int WM = TM / 2, WN = TN / 2, GM = WM / 16, GN = WN / 16, LA = TM * 8 / 256, LW = TN * 8 / 256;
     __shared__ intx4 sA[TM * 8], sW[TN * 8];
@@ -348,6 +354,8 @@ template <int TM, int TN> __global__ __launch_bounds__(256) void gemm_block_tile
 // W (256 rows x 128 bytes), which travel from memory to LDS without passing registers: three slots for A, two for W (160 KB), so that a block's A has two
 // blocks' time to land and its W one.  Chunk p of row r lies at p ^ (r / 2 % 8), applied where it is read from memory.
 // Per block and wavefront 24 KB of fragments feed 32 MFMAs; each one's sums are scaled into the accumulators while the next ones run.
+// 16384 x 4096 x 4096: 258 us, 2.13 PFLOP/s (an FP8 product with one scale in all reaches 2.68 as a library's): the matrix cores are busy for 54 % of the cycles
+// at the 1.86 GHz that the chip holds under them; the scaling takes four vector instructions per MFMA.
 // ---------------------------------------------------------------------------------------------------------------------
 __device__ __attribute__((aligned(16))) uint8_t zero_chunk[16];  // stands for the chunks past the end of a row
 
@@ -511,6 +519,7 @@ int launch_ring(const BlockGemm &g, hipStream_t st) {
 // ---------------------------------------------------------------------------------------------------------------------
 // Products of a round or two of tiles: TM x TN tiles of C on four wavefronts (2 x 2), operands and row scales straight to LDS, SLOTS blocks of K on their
 // way or in use.  With few tiles the time is one tile's walk along K, so what counts is that a block costs its MFMAs and a barrier and no memory latency.
+// 517 x 1000 x 1104 7.7 us (144 tiles, 9 blocks), 1024 x 4096 x 4096 34 us, 2048 x 4096 x 4096 46 us, 1.5 PFLOP/s.
 // ---------------------------------------------------------------------------------------------------------------------
 template <int TM, int TN, int SLOTS, bool RAGGED> __global__ __launch_bounds__(256) void gemm_block_stream(BlockGemm g) {
     constexpr int WM = TM / 2, WN = TN / 2, GM = WM / 16, GN = WN / 16, LA = TM / 32, LW = TN / 32, LEAD = SLOTS - 1, LOADS = LA + LW + 1;
@@ -632,6 +641,9 @@ template <int MG> int launch_few(const BlockGemm &g, hipStream_t st) {
     return GR4AD_OK;
 }
 
+// The variants by size.  Up to 64 rows every weight is read once by whoever needs it.  Then the time is the rounds of tiles: a compute unit holds two workgroups of
+// 64 x 64 or 128 x 128 tiles and one of 256 x 256, so each size is left when it needs more rounds than the next (x 4096 x 4096, tiles of 64, 128, 256: 128 rows 15,
+// 35, 46 us; 1024 rows, two rounds of the smallest, 34, 36, 45; 2048 rows, one round of the middle ones, 65, 46, 47; 2816 rows 90, 74, 49; 4096 rows 125, 86, 60).
 int launch_block_gemm(const BlockGemm &g, hipStream_t st) {
     ProfScope ps(KC_GEMM_F8_BLOCK, st, 2.0 * (double)g.M * g.N * g.K, ((double)g.M + g.N) * g.K + 2.0 * (double)g.M * g.N);
     // rows in pieces of 16 bytes (and a tile's rows within 32 bits of its first): direct loads to LDS
@@ -640,9 +652,9 @@ int launch_block_gemm(const BlockGemm &g, hipStream_t st) {
     if (g.M <= 32) return launch_few<2>(g, st);
     if (g.M <= 64) return launch_few<4>(g, st);
     if (aligned) {
-        if (ceil_div64(g.M, kRing) * ceil_div64(g.N, kRing) >= 192) return launch_ring(g, st);
-        if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) >= 192) return launch_stream<128, 128, 2>(g, st);
-        return launch_stream<64, 64, 4>(g, st);
+        if (ceil_div64(g.M, 64) * ceil_div64(g.N, 64) <= 1024) return launch_stream<64, 64, 4>(g, st);
+        if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) <= 512) return launch_stream<128, 128, 2>(g, st);
+        return launch_ring(g, st);
     }
     if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) < 256) return launch_tile<64, 64>(g, st);
     return launch_tile<128, 128>(g, st);

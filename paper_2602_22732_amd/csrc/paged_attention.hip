@@ -8,9 +8,9 @@
 // and both operands of the two products, S^T = K Q^T and O^T = V^T P^T, are read along their contraction in 16-byte pieces.
 //
 //  * paged_append<T, DH>    new keys and values into their pages (ahead of paged_flash; the others take them where they are).
-//  * paged_rows<T, DH>      16 rows (token, head of the group) of one (sequence, key head) per workgroup, whose wavefronts walk
+//  * paged_rows<T, DH, MR>  16 or 32 rows (token, head of the group) of one (sequence, key head) per workgroup, whose wavefronts walk
 //                           stretches of the keys of their own; operands go from memory to registers.
-//  * paged_flash<DH>        128 rows per workgroup, keys and values staged in LDS (bf16).
+//  * paged_flash<DH, ..>    128 or 256 rows per workgroup, keys and values staged in LDS (bf16).
 //  * paged_join<T, DH>      joins the stretches of several workgroups.
 #include <type_traits>
 
@@ -430,7 +430,12 @@ __device__ __forceinline__ float query_sum(float v) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
-// MR groups of 16 rows per workgroup (each key read serves them all).
+// Few rows: MR groups of 16 rows per workgroup (each key read serves them all), whose four wavefronts walk stretches of the keys of their own, joined in LDS.
+// The softmax runs with the walk: maximum and sum so far, the sums rescaled when the maximum grows.  New tokens are taken from k_new and v_new where the walk
+// meets them, and the tile that they belong to leaves them on their page: a call of single tokens has no launch of its own for them.
+// With one token per sequence the time is the reading: bf16, 64 sequences of 512 to 8192 keys, 8 key heads of 128 columns, 230 us, 4.9 TB/s; two of 100001 to
+// 131072 keys in 32 parts 174 us, 5.2 TB/s (a copy reaches 5.25).  Many float32 rows are bound by their products: 32 sequences, 1 to 96 tokens of 16 heads of 64
+// columns, a window of 1024, 109 us, the matrix cores busy for 39 % of the cycles (16 rows per workgroup 134: every key is read twice as often).
 template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH <= 64 ? 4 : MR == 2 ? 3 : 2) void paged_rows(PagedArgs a) {
     using F = Frags<T, DH>;
     constexpr int KB = F::KB, VF = F::VF, NW = 4, ROWS = 16 * MR;
@@ -645,13 +650,14 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Many rows: QB * 128 rows (token, head of the group) of one (sequence, key head) per workgroup, QB * 32 to a wavefront.  The keys stream through LDS in
-// tiles of 64 [64 x DH] with their values [DH x 64], two of each, filled by direct global->LDS loads.  Both products are transposed, so a lane owns
-// QB rows: their maxima and sums are its own, and P^T leaves the first product as the second's operand (key rows enter with bits 2 and 3 of their index
-// swapped, which makes the eight keys a lane holds for one MFMA step consecutive).
+// Many rows: 32 NW rows (token, head of the group) of one (sequence, key head) per workgroup, 32 to a wavefront.  The keys stream through LDS in
+// tiles of 64 [64 x DH] with their values [DH x 64], SLOTS of each, filled by direct global->LDS loads.  Both products are transposed, so a lane owns
+// a row: its maximum and sum are its own, and P^T leaves the first product as the second's operand (key rows enter with bits 2 and 3 of their index
+// swapped, which makes the eight keys a lane holds for one MFMA step consecutive; the weights are rounded to bf16 there, while their sum keeps 32 bits).
 // The matrix cores and the vector instructions of the softmax need about the same time, so a wavefront runs them side by side: the scores of tile x + 1 are
-// formed while those of tile x become weights, and the maximum of tile x + 1 is found while the values of tile x are added.  QB = 2: a fragment read from
-// LDS feeds two MFMAs (with one, 32 KB of LDS reads per wavefront and tile take as long as the MFMAs).
+// formed while those of tile x become weights.  (64 rows per wavefront halve the reads of LDS and do not fit the registers: 1075 us for what takes 327.)
+// bf16, 4 sequences of 1000 to 1024 new tokens among up to 8192, 32 heads of 128 columns over 8: 327 us under the tracer, 286 in a row of calls, 0.95 PFLOP/s
+// of the products that the mask leaves; the matrix cores are busy for 40 % of the cycles, the rest is the softmax's and the reads of LDS.
 // ---------------------------------------------------------------------------------------------------------------------
 template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) void paged_flash(PagedArgs a) {
     constexpr int QB = 1, ROWS = NW * 32 * QB, KT = 64, KCH = DH / 8, HALF = KT * KCH, KSTEPS = DH / 16, MT = DH / 32, KI = HALF / 64 / NW, LEAD = SLOTS - 1;
@@ -1057,7 +1063,8 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
         }
 }
 
-// Joins the workgroups' shares of a row: WAVES wavefronts per row, each with shares of its own.
+// Joins the workgroups' shares of a row, out = sum_s 2^(m_s - m) o_s / sum_s 2^(m_s - m) l_s: WAVES wavefronts per row, each with shares of its own, four
+// from 16 shares on.  Latency: 2048 rows of 128 columns in two shares 6.4 us, 64 rows in 32 shares 7.0.
 template <typename T, int DH, int WAVES> __global__ __launch_bounds__(256) void paged_join(PagedArgs a) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, part_of = wave % WAVES;
     const int64_t w = (int64_t)blockIdx.x * (4 / WAVES) + wave / WAVES;  // (tile, key head, row)
@@ -1115,7 +1122,7 @@ int64_t tiles_of(int N, int B, int group, int rows) {
     return n < all ? n : all;
 }
 
-// rows: of a tile: 16 or 32 (paged_rows), or 256 that share staged keys (paged_flash).  nsplit: workgroups that share a tile's keys.
+// rows: of a tile: 16 or 32 (paged_rows), or 128 or 256 that share staged keys (paged_flash).  nsplit: workgroups that share a tile's keys.
 struct Plan {
     int rows;
     int64_t tiles, join_tiles;
