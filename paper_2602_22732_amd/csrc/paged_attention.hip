@@ -251,7 +251,14 @@ __device__ __forceinline__ int page_numbers(const PagedArgs &a, int b, int first
 // A lane holds row lane % 16 of the first operand and c = lane / 16 says which part of the contraction; of S^T it gets query lane % 16 and four rows.
 // bf16: key rows enter in an order that makes the eight keys a lane then holds of P consecutive, as its piece of V^T has them.
 // New tokens among a block's keys, [first, end) of it: k, v are where its key 0 would lie among their rows
-template <typename T> struct NewRows { const T *k, *v; int64_t stride; int first, end, keep_from, keep_to; };  // [keep_from, keep_to]: keys this workgroup writes
+template <typename T> struct NewRows {
+    const T *k, *v;
+    int64_t stride;
+    int first, end, keep_from, keep_to;  // [keep_from, keep_to]: keys this workgroup writes
+    __device__ __forceinline__ bool has(int key) const { return key >= first && key < end; }
+    __device__ __forceinline__ bool keeps(int key) const { return key >= keep_from && key <= keep_to; }
+    __device__ __forceinline__ int near(int key) const { return min(max(key, first), end - 1); }  // itself if it is new, otherwise one that is
+};
 template <typename T, int DH> struct Frags;
 template <int DH> struct Frags<bf16, DH> {
     static constexpr int KB = 32, KF = (DH + 31) / 32, VF = DH / 16;
@@ -313,29 +320,40 @@ template <int DH> struct Frags<bf16, DH> {
     __device__ __forceinline__ void take_new(const NewRows<bf16> &n, bf16 *k0, bf16 *k1, bf16 *v0, bf16 *v1, int valid, int page) {
         const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
 #pragma unroll
-        for (int u = 0; u < 2; u++) {
+        for (int u = 0; u < 2; u++) {  // (all of a row from one place or the other, without a branch)
             const int key = key_of(u, r);
-            if (key < n.first || key >= n.end || 8 * c >= DH) continue;
-            const bf16 *src = n.k + (int64_t)key * n.stride + 8 * c;
-            bf16 *dst = (r < 8 ? k0 : k1) + (key % 16) * DH + 8 * c;
-            const bool keep = key >= n.keep_from && key <= n.keep_to;
+            const bf16 *src = (n.has(key) ? n.k + (int64_t)key * n.stride : (r < 8 ? k0 : k1) + (key % 16) * DH) + 8 * c;
 #pragma unroll
-            for (int f = 0; f < KF; f++) {
-                k[u][f] = *(const bf16x8 *)(src + 32 * f);
-                if (keep && (valid >> (key / 16) & 1)) *(bf16x8 *)(dst + 32 * f) = k[u][f];
-            }
+            for (int f = 0; f < KF; f++)
+                if (DH % 32 == 0 || 8 * c < DH) k[u][f] = *(const bf16x8 *)(src + 32 * f);
         }
         bf16 *dst = (c < 2 ? v0 : v1) + (8 * c) % 16 + r * page;
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
+        for (int e = 0; e < 8; e += 2) {  // two keys' values are requested together
             const int key = 8 * c + e;
-            if (key < n.first || key >= n.end) continue;
-            const bool keep = key >= n.keep_from && key <= n.keep_to;
+            if (!n.has(key) && !n.has(key + 1)) continue;
+            bf16 x[2][VF];
 #pragma unroll
-            for (int t = 0; t < VF; t++) {
-                v[t][e] = n.v[(int64_t)key * n.stride + 16 * t + r];
-                if (keep && (valid >> (key / 16) & 1)) dst[16 * t * page + e] = v[t][e];
+            for (int i = 0; i < 2; i++)
+#pragma unroll
+                for (int t = 0; t < VF; t++) x[i][t] = n.v[(int64_t)n.near(key + i) * n.stride + 16 * t + r];
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const bool has = n.has(key + i), keep = has && n.keeps(key + i) && (valid >> (key / 16) & 1);
+#pragma unroll
+                for (int t = 0; t < VF; t++) {
+                    v[t][e + i] = has ? x[i][t] : v[t][e + i];
+                    if (keep) dst[16 * t * page + e + i] = x[i][t];
+                }
             }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+            const int key = key_of(u, r);
+            bf16 *dk = (r < 8 ? k0 : k1) + (key % 16) * DH + 8 * c;
+            if (n.has(key) && n.keeps(key) && (valid >> (key / 16) & 1) && 8 * c < DH)
+#pragma unroll
+                for (int f = 0; f < KF; f++) *(bf16x8 *)(dk + 32 * f) = k[u][f];
         }
     }
     // values of keys nobody in the tile may use (slots behind the last token, pages that do not exist): out of the product
@@ -386,25 +404,31 @@ template <int DH> struct Frags<float, DH> {
     }
     __device__ __forceinline__ void take_new(const NewRows<float> &n, float *k0, float *, float *v0, float *, int valid, int page) {
         const int r = threadIdx.x % 16, c = threadIdx.x % 64 / 16;
-        if (r >= n.first && r < n.end) {
-            const bool keep = r >= n.keep_from && r <= n.keep_to;
+        const float *src = (n.has(r) ? n.k + (int64_t)r * n.stride : k0 + r * DH) + 4 * c;
 #pragma unroll
-            for (int f = 0; f < KF; f++) {
-                k[f] = *(const floatx4 *)(n.k + (int64_t)r * n.stride + 16 * f + 4 * c);
-                if (keep && valid) *(floatx4 *)(k0 + r * DH + 16 * f + 4 * c) = k[f];
+        for (int f = 0; f < KF; f++) k[f] = *(const floatx4 *)(src + 16 * f);
+        constexpr int AT_ONCE = DH > 64 ? 1 : 4;  // keys whose values are requested before any is used, without a branch (as many as the registers take)
+#pragma unroll
+        for (int e0 = 0; e0 < 4; e0 += AT_ONCE) {
+            float x[AT_ONCE][VF];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; i++)
+#pragma unroll
+                for (int t = 0; t < VF; t++) x[i][t] = n.v[(int64_t)n.near(4 * c + e0 + i) * n.stride + 16 * t + r];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; i++) {
+                const int key = 4 * c + e0 + i;
+                const bool has = n.has(key), keep = has && n.keeps(key) && valid;
+#pragma unroll
+                for (int t = 0; t < VF; t++) {
+                    v[t][e0 + i] = has ? x[i][t] : v[t][e0 + i];
+                    if (keep) v0[(16 * t + r) * page + key] = x[i][t];
+                }
             }
         }
+        if (n.has(r) && n.keeps(r) && valid)
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const int key = 4 * c + e;
-            if (key < n.first || key >= n.end) continue;
-            const bool keep = key >= n.keep_from && key <= n.keep_to;
-#pragma unroll
-            for (int t = 0; t < VF; t++) {
-                v[t][e] = n.v[(int64_t)key * n.stride + 16 * t + r];
-                if (keep && valid) v0[(16 * t + r) * page + key] = v[t][e];
-            }
-        }
+            for (int f = 0; f < KF; f++) *(floatx4 *)(k0 + r * DH + 16 * f + 4 * c) = k[f];
     }
     __device__ __forceinline__ void drop_values(int from, int valid) {
         const int c = threadIdx.x % 64 / 16;
@@ -430,13 +454,14 @@ __device__ __forceinline__ float query_sum(float v) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
-// Few rows: MR groups of 16 rows per workgroup (each key read serves them all), whose four wavefronts walk stretches of the keys of their own, joined in LDS.
+// Few rows: MR groups of 16 rows per workgroup (each key read serves them all), whose four wavefronts walk blocks of the keys in turn, joined in LDS.
 // The softmax runs with the walk: maximum and sum so far, the sums rescaled when the maximum grows.  New tokens are taken from k_new and v_new where the walk
 // meets them, and the tile that they belong to leaves them on their page: a call of single tokens has no launch of its own for them.
-// With one token per sequence the time is the reading: bf16, 64 sequences of 512 to 8192 keys, 8 key heads of 128 columns, 230 us, 4.9 TB/s; two of 100001 to
-// 131072 keys in 32 parts 174 us, 5.2 TB/s (a copy reaches 5.25).  Many float32 rows are bound by their products: 32 sequences, 1 to 96 tokens of 16 heads of 64
-// columns, a window of 1024, 109 us, the matrix cores busy for 39 % of the cycles (16 rows per workgroup 134: every key is read twice as often).
-template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH <= 64 ? 4 : MR == 2 ? 3 : 2) void paged_rows(PagedArgs a) {
+// With one token per sequence the time is the reading: bf16, 64 sequences of 512 to 8192 keys, 8 key heads of 128 columns, 217 us, 5.2 TB/s; two of 100001 to
+// 131072 keys in 32 parts 164 us, 5.7 TB/s (a copy reaches 5.25).  Many float32 rows are bound by their products: 16 sequences of 300 tokens over 4000, 16 heads of
+// 64 columns, 741 us, 0.1 PFLOP/s, three quarters of a large product's rate; 32 heads of 128 columns 2960 (16 rows per workgroup 4170: every key is read twice as
+// often).  Where 840 tiles meet 768 places, as with 32 sequences, 1 to 96 tokens of 16 heads of 64 columns and a window of 1024 (101 us), half of that.
+template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH <= 64 ? 4 : MR == 2 && DH <= 64 ? 3 : 2) void paged_rows(PagedArgs a) {
     using F = Frags<T, DH>;
     constexpr int KB = F::KB, VF = F::VF, NW = 4, ROWS = 16 * MR;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), n = lane % 16, c = lane / 16;
@@ -447,7 +472,11 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
     const int p_lo = base + R0 / a.group, p_hi = base + (R1 - 1) / a.group;
     const Blocks bl = visible_blocks<KB>(a, p_lo, p_hi);
     const int each = (bl.count + a.nsplit * NW - 1) / (a.nsplit * NW);
-    const int x0 = min((split * NW + wave) * each, bl.count), x1 = min(x0 + each, bl.count);
+    // The wavefronts take the workgroup's blocks [y0, y1) in turn, so that each has its share of the new tokens, which cost more (16 sequences of 300 float32 tokens
+    // over 4000: 3150 us with stretches of their own, 2960 in turn; two tokens over 100001 to 131072 172 and 164).  Of a few blocks they take stretches: the last
+    // wavefront, which meets the new token, then has the fewest (one token over 777: 10 us, 11.2 in turn; the widest kind has no register left for the choice).
+    const int y0 = min(split * NW * each, bl.count), y1 = min(y0 + NW * each, bl.count);
+    const int step = MR * DH <= 128 && each <= 16 ? 1 : NW, x0 = step == 1 ? min(y0 + wave * each, y1) : y0 + wave, x1 = step == 1 ? min(x0 + each, y1) : y1;
 
     int p[MR];
     typename F::Q q[MR];
@@ -516,7 +545,7 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
 #pragma unroll
         for (int i = 0; i < MR; i++) f.scores(sc[i], q[i]);
         if constexpr (NEXT) {
-            src = source(x + 1);
+            src = source(x + step);
             f.load_k(src.k0, src.k1);
         }
         const bool whole = valid == 3 && key0 + KB - 1 <= p_lo && (!a.window || p_hi - key0 < a.window || key0 + KB <= a.sinks);
@@ -591,13 +620,13 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
             xn = min(max(first < bl.first ? first : max(bl.first, first - bl.from + bl.first), x0), x1);
         }
         int x = x0;
-        for (; x < xn && x + 1 < x1; x++) block(yes, no, x);
-        for (; x + 1 < x1; x++) block(yes, yes, x);
+        for (; x < xn && x + step < x1; x += step) block(yes, no, x);
+        for (; x + step < x1; x += step) block(yes, yes, x);
         if (x < xn) block(no, no, x);
         else block(no, yes, x);
     }
 
-    // the wavefronts' stretches, joined in their order, 16 rows at a time
+    // the wavefronts' shares, joined in their order, 16 rows at a time
     const PagedArgs z = late_args();
     __shared__ float sm[NW][16], sl[NW][16];
     __shared__ __attribute__((aligned(16))) float so[NW][16][DH + 4];
@@ -641,7 +670,6 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
         }
     }
     if (__syncthreads_or(bad)) {
-        const int y0 = min(split * NW * each, bl.count), y1 = min(y0 + NW * each, bl.count);
         for (int r = wave; r < R1 - R0; r += NW) {
             const int RR = R0 + r, tk = RR / z.group;
             plain_row<T, DH, KB>(z, s, bl, y0, y1, kvh, s.start + tk, kvh * z.group + RR - tk * z.group, base + tk, split);
@@ -1135,7 +1163,7 @@ Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, 
     const int group = H / Hkv;
     const int64_t rows = ceil_div64((int64_t)N * group, B);  // of a sequence and key head, on average
     if (dtype == GR4AD_BF16 && dh >= 32 && (rows >= 48 || (dh == 128 && rows > 16))) p.rows = rows > 128 ? kFlashRows : kHalfFlashRows;
-    else p.rows = rows <= 16 || dh > 64 ? 16 : 32;  // (32 rows of 128 columns do not fit the registers)
+    else p.rows = rows <= 16 ? 16 : 32;
     p.tiles = tiles_of(N, B, group, p.rows);
     p.join_tiles = tiles_of(N, B, group, kRows);
     const bool flash = p.flash();
@@ -1175,7 +1203,8 @@ template <typename T, int DH> int launch_rows(const PagedArgs &a, const Plan &p,
     if (p.rows == 16) {
         hipLaunchKernelGGL((paged_rows<T, DH, 1>), dim3((unsigned)grid), dim3(256), 0, st, a);
     } else if (p.rows == 32) {
-        if constexpr (DH <= 64) hipLaunchKernelGGL((paged_rows<T, DH, 2>), dim3((unsigned)grid), dim3(256), 0, st, a);
+        // (more than 16 bf16 rows of 128 columns are always staged)
+        if constexpr (DH <= 64 || sizeof(T) == 4) hipLaunchKernelGGL((paged_rows<T, DH, 2>), dim3((unsigned)grid), dim3(256), 0, st, a);
     } else if constexpr (sizeof(T) == 2 && DH >= 32) {
         // (half the rows: two workgroups share a compute unit and its LDS)
         const int s = p.rows == kFlashRows ? launch_flash<DH, kFlashRows / 32, 4>(a, (unsigned)grid, st) : launch_flash<DH, kHalfFlashRows / 32, DH == 128 ? 2 : 4>(a, (unsigned)grid, st);

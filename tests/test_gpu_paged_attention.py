@@ -338,3 +338,10 @@ def test_two_streams_at_once():
         want, tol = c.expected()
         assert all(same(g, got[0]) for g in got)
         assert ((got[0].cpu().double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dh,page", [(128, 16), (128, 64), (64, 16)])
+def test_float32_chunks(dh, page):
+    c = Case("f32", dh, 8, 2, page, new=[60, 1, 17, 0, 3], lens=[500, 200, 17, 30, 1400], seed=21)
+    check(c)
+    check(c, window=90, sinks=5)
