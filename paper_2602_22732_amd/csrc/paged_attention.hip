@@ -460,7 +460,7 @@ __device__ __forceinline__ float query_sum(float v) {
 // With one token per sequence the time is the reading: bf16, 64 sequences of 512 to 8192 keys, 8 key heads of 128 columns, 217 us, 5.2 TB/s; two of 100001 to
 // 131072 keys in 32 parts 164 us, 5.7 TB/s (a copy reaches 5.25).  Many float32 rows are bound by their products: 16 sequences of 300 tokens over 4000, 16 heads of
 // 64 columns, 741 us, 0.1 PFLOP/s, three quarters of a large product's rate; 32 heads of 128 columns 2960 (16 rows per workgroup 4170: every key is read twice as
-// often).  Where 840 tiles meet 768 places, as with 32 sequences, 1 to 96 tokens of 16 heads of 64 columns and a window of 1024 (101 us), half of that.
+// often).  Where 832 tiles meet 768 places, as with 32 sequences, 1 to 96 tokens of 16 heads of 64 columns and a window of 1024 (101 us), half of that.
 template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH <= 64 ? 4 : MR == 2 && DH <= 64 ? 3 : 2) void paged_rows(PagedArgs a) {
     using F = Frags<T, DH>;
     constexpr int KB = F::KB, VF = F::VF, NW = 4, ROWS = 16 * MR;
@@ -684,7 +684,7 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
 // swapped, which makes the eight keys a lane holds for one MFMA step consecutive; the weights are rounded to bf16 there, while their sum keeps 32 bits).
 // The matrix cores and the vector instructions of the softmax need about the same time, so a wavefront runs them side by side: the scores of tile x + 1 are
 // formed while those of tile x become weights.  (64 rows per wavefront halve the reads of LDS and do not fit the registers: 1075 us for what takes 327.)
-// bf16, 4 sequences of 1000 to 1024 new tokens among up to 8192, 32 heads of 128 columns over 8: 327 us under the tracer, 286 in a row of calls, 0.95 PFLOP/s
+// bf16, 4 sequences of 1000 to 1024 new tokens among up to 8192, 32 heads of 128 columns over 8: 314 us under the tracer, 280 in a row of calls, 0.97 PFLOP/s
 // of the products that the mask leaves; the matrix cores are busy for 40 % of the cycles, the rest is the softmax's and the reads of LDS.
 // ---------------------------------------------------------------------------------------------------------------------
 template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) void paged_flash(PagedArgs a) {
@@ -1168,9 +1168,9 @@ Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, 
     p.join_tiles = tiles_of(N, B, group, kRows);
     const bool flash = p.flash();
     // Workgroups enough to fill the chip (counted as if all sequences had the same number of rows): one per compute unit for tiles of 256 rows, two for the
-    // others (tiles of 32 rows, 840 of them: 130 us alone, 136 in halves with their join); with tiles of 16 rows, which stand for many sequences of their
-    // own lengths, four where that many are near (512 of up to 8192 keys: alone 261 us, in halves 233, in quarters 238; 16 of 100000 keys in 16 parts 175 us, in
-    // 64 parts 189).  A part has 256 keys at least (1024 of the staged kinds), and a tile of 16 rows with 256 KB of keys and values at most stays whole: the parts would wait
+    // others (tiles of 32 rows, 832 of them: 102 us alone, 113 in halves with their join); with tiles of 16 rows, which stand for many sequences of their own
+    // lengths, four where that many are near (512 of up to 8192 keys: alone 256 us, in halves 224, in quarters 236; 16 of 131072 keys in 16 parts 176 us, in 32 parts
+    // 172, in 64 parts 190).  A part has 256 keys at least (1024 of the staged kinds), and a tile of 16 rows with 256 KB of keys and values at most stays whole: the parts would wait
     // longer for their join than they save (one row of 777 keys, calls in a row: bf16 of 64 columns 9.8 us against 14.7; fp32 of 128, twice beyond: 23.4 against 15.2).
     const int64_t blocks = (int64_t)B * ceil_div64(rows, p.rows) * Hkv, enough = p.rows == kFlashRows ? 256 : p.rows == 16 && blocks >= 256 ? 1024 : 512, least = flash ? 1024 : 256;
     int64_t keys = (int64_t)max_pages * page;
