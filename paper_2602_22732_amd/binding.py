@@ -446,7 +446,8 @@ def _ptr(t):
 
 def op_paged_attention(q, k_pages, v_pages, page_table, q_start, seq_len, k_new=None, v_new=None, scale=None, window=0, sinks=0, out=None, workspace=None, stream=None):
     """gr4ad_op_paged_attention: q [N,H,dh] (rows may be strided), k_pages [n_pages,H_kv,page_size,dh], v_pages [n_pages,H_kv,dh,page_size], page_table
-    [B,max_pages], q_start [B+1], seq_len [B] int32; k_new, v_new [N,H_kv,dh] are written into their pages first.  scale: 1/sqrt(dh) if None."""
+    [B,max_pages], q_start [B+1], seq_len [B] int32; k_new, v_new [N,H_kv,dh] are written into their pages first (pages that no other sequence of the call
+    has in its table).  scale: 1/sqrt(dh) if None."""
     what = "op_paged_attention"
     at = _place(what, q, stream, (k_pages, v_pages, page_table, q_start, seq_len, k_new, v_new, out, workspace))
     if at is not None:
@@ -474,6 +475,8 @@ def op_paged_attention(q, k_pages, v_pages, page_table, q_start, seq_len, k_new=
         if t.dtype is not dtype or t.shape != (N, heads, dh) or one != 1 or (heads > 1 and head != dh):
             raise ValueError("%s: %s must be %s [%d,%d,%d] with dense rows, got %s %s strides %s" % (what, name, dtype, N, heads, dh, t.dtype, tuple(t.shape), t.stride()))
         strides.append(row if N > 1 else heads * dh)
+    if window >= 1 << 31 or sinks >= 1 << 31:
+        raise ValueError("%s: window %d, sinks %d" % (what, window, sinks))
     if k_new is not None and v_new is not None and strides[1] != strides[2]:
         raise ValueError("%s: rows of k_new and v_new lie %d and %d values apart" % (what, strides[1], strides[2]))
     L = lib()

@@ -689,6 +689,7 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
 // ---------------------------------------------------------------------------------------------------------------------
 template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) void paged_flash(PagedArgs a) {
     constexpr int QB = 1, ROWS = NW * 32 * QB, KT = 64, KCH = DH / 8, HALF = KT * KCH, KSTEPS = DH / 16, MT = DH / 32, KI = HALF / 64 / NW, LEAD = SLOTS - 1;
+    static_assert(KI * 64 * NW == HALF, "every wavefront loads as much of a tile");
     extern __shared__ bf16x8 smem[];  // keys of SLOTS tiles, values of SLOTS tiles: HALF chunks each
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), frow = lane % 32, hf = lane / 32;
     const int split = blockIdx.x / a.Hkv % a.nsplit, kvh = blockIdx.x % a.Hkv, page = 1 << a.page_shift;
@@ -1162,7 +1163,7 @@ Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, 
     Plan p;
     const int group = H / Hkv;
     const int64_t rows = ceil_div64((int64_t)N * group, B);  // of a sequence and key head, on average
-    if (dtype == GR4AD_BF16 && dh >= 32 && (rows >= 48 || (dh == 128 && rows > 16))) p.rows = rows > 128 ? kFlashRows : kHalfFlashRows;
+    if (dtype == GR4AD_BF16 && dh >= 32 && (rows >= 48 || (dh == 128 && rows > 16))) p.rows = rows > 128 && dh > 32 ? kFlashRows : kHalfFlashRows;  // (a tile of 32 columns is one load for each of four wavefronts)
     else p.rows = rows <= 16 ? 16 : 32;
     p.tiles = tiles_of(N, B, group, p.rows);
     p.join_tiles = tiles_of(N, B, group, kRows);
@@ -1207,7 +1208,9 @@ template <typename T, int DH> int launch_rows(const PagedArgs &a, const Plan &p,
         if constexpr (DH <= 64 || sizeof(T) == 4) hipLaunchKernelGGL((paged_rows<T, DH, 2>), dim3((unsigned)grid), dim3(256), 0, st, a);
     } else if constexpr (sizeof(T) == 2 && DH >= 32) {
         // (half the rows: two workgroups share a compute unit and its LDS)
-        const int s = p.rows == kFlashRows ? launch_flash<DH, kFlashRows / 32, 4>(a, (unsigned)grid, st) : launch_flash<DH, kHalfFlashRows / 32, DH == 128 ? 2 : 4>(a, (unsigned)grid, st);
+        int s = GR4AD_OK;
+        if (p.rows == kHalfFlashRows) s = launch_flash<DH, kHalfFlashRows / 32, DH == 128 ? 2 : 4>(a, (unsigned)grid, st);
+        else if constexpr (DH > 32) s = launch_flash<DH, kFlashRows / 32, 4>(a, (unsigned)grid, st);
         if (s) return s;
     }
     GR4AD_LAUNCH_CHECK();

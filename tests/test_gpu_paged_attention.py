@@ -345,3 +345,12 @@ def test_float32_chunks(dh, page):
     c = Case("f32", dh, 8, 2, page, new=[60, 1, 17, 0, 3], lens=[500, 200, 17, 30, 1400], seed=21)
     check(c)
     check(c, window=90, sinks=5)
+
+
+@pytest.mark.parametrize("dh,H,H_kv,page", [(32, 4, 2, 16), (32, 2, 1, 128), (64, 4, 1, 16), (128, 4, 1, 64)])
+def test_chunks_among_finite_values(dh, H, H_kv, page):
+    # no value anywhere is a NaN, and what the compute units' local memory holds from before is finite too: a tile that was not loaded shows as a wrong result
+    assert torch.isfinite(run(Case("bf16", 128, 8, 1, 64, new=[300] * 40, lens=[320] * 40, seed=22, stale=0.25), 0, 0, True)[0].float()).all()
+    c = Case("bf16", dh, H, H_kv, page, new=[300, 40], lens=[1000, 41], seed=23, stale=0.25)
+    check(c)
+    check(c, window=300, sinks=3)

@@ -108,6 +108,9 @@ def test_binding_refuses_types_shapes_and_strides():
         binding.op_paged_attention(**good, k_new=z(3, 2, 64))
     with pytest.raises(ValueError):
         binding.op_paged_attention(**good, out=z(3, 4, 64, dtype=torch.bfloat16))
+    for kw in (dict(window=1 << 32), dict(window=4, sinks=1 << 31)):
+        with pytest.raises(ValueError):
+            binding.op_paged_attention(**good, **kw)
     with pytest.raises(ValueError):
         binding.op_quantize_blocks(z(4, 8).t())
     with pytest.raises(ValueError):
