@@ -683,7 +683,7 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
 // a row: its maximum and sum are its own, and P^T leaves the first product as the second's operand (key rows enter with bits 2 and 3 of their index
 // swapped, which makes the eight keys a lane holds for one MFMA step consecutive; the weights are rounded to bf16 there, while their sum keeps 32 bits).
 // The matrix cores and the vector instructions of the softmax need about the same time, so a wavefront runs them side by side: the scores of tile x + 1 are
-// formed while those of tile x become weights.  (64 rows per wavefront halve the reads of LDS and do not fit the registers: 1075 us for what takes 327.)
+// formed while those of tile x become weights.  (64 rows per wavefront halve the reads of LDS and do not fit the registers: 1075 us for what takes 314.)
 // bf16, 4 sequences of 1000 to 1024 new tokens among up to 8192, 32 heads of 128 columns over 8: 314 us under the tracer, 280 in a row of calls, 0.97 PFLOP/s
 // of the products that the mask leaves; the matrix cores are busy for 40 % of the cycles, the rest is the softmax's and the reads of LDS.
 // ---------------------------------------------------------------------------------------------------------------------

@@ -354,3 +354,13 @@ def test_chunks_among_finite_values(dh, H, H_kv, page):
     c = Case("bf16", dh, H, H_kv, page, new=[300, 40], lens=[1000, 41], seed=23, stale=0.25)
     check(c)
     check(c, window=300, sinks=3)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dh,H,H_kv,page", [(16, 4, 2, 16), (32, 4, 1, 32), (64, 6, 1, 64), (128, 8, 2, 16), (128, 8, 1, 1024)])
+@pytest.mark.parametrize("new,lens", [([1, 1, 2], [1, 700, 90]), ([1, 1], [40, 3000]), ([30, 9], [400, 9]), ([90, 60, 1], [90, 800, 33])])
+def test_all_kinds_among_finite_values(dtype, dh, H, H_kv, page, new, lens):
+    # with the test above: no tile may be right only because a NaN sent its rows to the plain form
+    c = Case(dtype, dh, H, H_kv, page, new=new, lens=lens, seed=24, stale=0.25)
+    check(c)
+    check(c, window=60, sinks=2)
