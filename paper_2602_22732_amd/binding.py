@@ -337,6 +337,8 @@ def op_linear(A, W, bias=None, out_f32=False, stream=None):
 def op_quantize_rows(x, stream=None):
     """x [rows, n] bf16 -> (q [rows, n] uint8 holding E4M3 bytes, scale [rows] float32)."""
     rows, n = x.shape
+    if (rows | n) >> 31:
+        _beyond("op_quantize_blocks", rows=rows, n=n)
     q = torch.empty(rows, n, dtype=torch.uint8, device=x.device)
     scale = torch.empty(rows, dtype=torch.float32, device=x.device)
     _check(lib().gr4ad_op_quantize_rows(x.data_ptr(), q.data_ptr(), scale.data_ptr(), rows, n, _stream_ptr(stream)))
@@ -440,6 +442,11 @@ def _dense(what, name, t, dtype, shape):
         raise ValueError("%s: %s must be dense %s %s, got %s %s%s" % (what, name, dtype, tuple(shape), t.dtype, tuple(t.shape), "" if t.is_contiguous() else " (strided)"))
 
 
+def _beyond(what, **sizes):
+    """ValueError: the library takes sizes of 32 bits, and ctypes would pass their low bits on."""
+    raise ValueError("%s: sizes beyond 32 bits (%s)" % (what, ", ".join("%s %d" % kv for kv in sizes.items())))
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -475,8 +482,10 @@ def op_paged_attention(q, k_pages, v_pages, page_table, q_start, seq_len, k_new=
         if t.dtype is not dtype or t.shape != (N, heads, dh) or one != 1 or (heads > 1 and head != dh):
             raise ValueError("%s: %s must be %s [%d,%d,%d] with dense rows, got %s %s strides %s" % (what, name, dtype, N, heads, dh, t.dtype, tuple(t.shape), t.stride()))
         strides.append(row if N > 1 else heads * dh)
-    if window >= 1 << 31 or sinks >= 1 << 31:
-        raise ValueError("%s: window %d, sinks %d" % (what, window, sinks))
+    if (N | H | dh | B | max_pages | n_pages | H_kv | page) >> 31:
+        _beyond(what, N=N, H=H, dh=dh, B=B, max_pages=max_pages, n_pages=n_pages, H_kv=H_kv, page=page)
+    if not (-1 << 31 <= window < 1 << 31 and -1 << 31 <= sinks < 1 << 31):
+        _beyond(what, window=window, sinks=sinks)
     if k_new is not None and v_new is not None and strides[1] != strides[2]:
         raise ValueError("%s: rows of k_new and v_new lie %d and %d values apart" % (what, strides[1], strides[2]))
     L = lib()
@@ -503,6 +512,8 @@ def op_quantize_blocks(x, block_rows=1, stream=None):
     if dtype not in (torch.float32, torch.bfloat16) or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1) or block_rows not in (1, 128):
         raise ValueError("op_quantize_blocks: x [rows, n] float32 or bfloat16 with dense rows, block_rows 1 or 128; got %s %s strides %s, %r" % (dtype, tuple(x.shape), x.stride(), block_rows))
     rows, n = x.shape
+    if (rows | n) >> 31:
+        _beyond("op_quantize_blocks", rows=rows, n=n)
     q = torch.empty(rows, n, dtype=torch.uint8, device=x.device)
     scale = torch.empty(-(-n // 128), -(-rows // block_rows), dtype=torch.float32, device=x.device)
     _check(lib().gr4ad_op_quantize_blocks(BF16 if dtype is torch.bfloat16 else F32, x.data_ptr(), x.stride(0) if rows > 1 else n, q.data_ptr(), scale.data_ptr(), rows, n, block_rows,
@@ -521,6 +532,8 @@ def op_linear_fp8_block(Aq, a_scale, Wq, w_scale, bias=None, out_dtype=torch.bfl
         raise ValueError("%s: Aq [M,K], Wq [N,K], out_dtype bfloat16 or float16" % what)
     M, K = Aq.shape
     N, nb = Wq.shape[0], -(-K // 128)
+    if (M | N | K) >> 31:
+        _beyond(what, M=M, N=N, K=K)
     _dense(what, "Aq", Aq, torch.uint8, (M, K))
     _dense(what, "Wq", Wq, torch.uint8, (N, K))
     _dense(what, "a_scale", a_scale, torch.float32, (nb, M))
@@ -550,15 +563,23 @@ def op_adjust_logits(logits, history=None, history_len=None, repetition=None, pr
     V = shape[-1]
     rows = logits.numel() // V if V else 0
     one = (rows,)
+    if (rows | V) >> 31:
+        _beyond(what, rows=rows, V=V)
     rules = LogitRules()
     if history is not None:
         _dense(what, "history", history, i32, (rows, history.shape[-1]))
+        if history.shape[1] >> 31:
+            _beyond(what, history=history.shape[1])
         rules.history, rules.history_stride = history.data_ptr(), history.shape[1]
     if bias is not None:
         _dense(what, "bias", bias, f32, (bias.shape[0], V))
+        if bias.shape[0] >> 31:
+            _beyond(what, bias=bias.shape[0])
         rules.bias, rules.n_bias = bias.data_ptr(), bias.shape[0]
     if mask is not None:
         _dense(what, "mask", mask, i32, (mask.shape[0], -(-V // 32)))
+        if mask.shape[0] >> 31:
+            _beyond(what, mask=mask.shape[0])
         rules.mask, rules.n_masks = mask.data_ptr(), mask.shape[0]
     if history_len is not None:
         _dense(what, "history_len", history_len, i32, one)

@@ -1,0 +1,49 @@
+"""What the operators on pages, FP8 blocks and logits promise beside their results, as far as the host decides it: sizes beyond 32 bits, buffers that overlap or are
+not dense, launches that do not fit, and what a failing call says."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2602_22732_amd import binding
+
+I32, U8 = torch.int32, torch.uint8
+
+
+@pytest.fixture
+def anywhere(monkeypatch):
+    """The binding's own checks on tensors that have a shape and no memory."""
+    monkeypatch.setattr(binding, "_place", lambda *_: None)
+    return lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device="meta")
+
+
+BIG = 2 ** 32  # a size of BIG + n would reach the library as n
+
+
+def test_sizes_that_32_bits_do_not_hold(anywhere):
+    z = anywhere
+    bf16 = torch.bfloat16
+    for x in (z(1, BIG + 128, dtype=bf16), z(BIG + 2, 3), z(2 ** 31, 1)):
+        with pytest.raises(ValueError, match="32 bits"):
+            binding.op_quantize_blocks(x)
+    for M, N, K in ((BIG + 3, 4, 128), (3, BIG + 4, 128), (3, 4, BIG + 128), (1, 1, 2 ** 31)):
+        with pytest.raises(ValueError, match="32 bits"):
+            binding.op_linear_fp8_block(z(M, K, dtype=U8), z(-(-K // 128), M), z(N, K, dtype=U8), z(-(-K // 128), -(-N // 128)))
+    for over in (dict(logits=z(BIG + 2, 8)), dict(logits=z(1, BIG + 8)), dict(history=z(2, BIG + 1, dtype=I32)), dict(bias=z(BIG + 1, 8)), dict(mask=z(BIG + 1, 1, dtype=I32))):
+        with pytest.raises(ValueError, match="32 bits"):
+            binding.op_adjust_logits(**dict(dict(logits=z(2, 8)), **over))
+
+
+@pytest.mark.parametrize("sizes", [dict(N=BIG + 1), dict(H=BIG + 2), dict(B=BIG + 1), dict(max_pages=BIG + 1), dict(n_pages=BIG + 1), dict(H_kv=BIG + 1, H=BIG + 1), dict(page=BIG + 16), dict(dh=BIG + 16)])
+def test_attention_sizes_that_32_bits_do_not_hold(anywhere, sizes):
+    z, s = anywhere, dict(dict(N=1, H=2, B=1, max_pages=1, n_pages=1, H_kv=1, page=16, dh=16), **sizes)
+    with pytest.raises(ValueError, match="32 bits"):
+        binding.op_paged_attention(z(s["N"], s["H"], s["dh"]), z(s["n_pages"], s["H_kv"], s["page"], s["dh"]), z(s["n_pages"], s["H_kv"], s["dh"], s["page"]), z(s["B"], s["max_pages"], dtype=I32),
+                                   z(s["B"] + 1, dtype=I32), z(s["B"], dtype=I32))
+
+
+@pytest.mark.parametrize("kw", [dict(window=BIG + 5), dict(window=5, sinks=BIG), dict(window=-BIG + 5), dict(window=5, sinks=-BIG)])
+def test_windows_that_32_bits_do_not_hold(anywhere, kw):
+    z = anywhere
+    with pytest.raises(ValueError, match="window"):
+        binding.op_paged_attention(z(1, 2, 16), z(1, 1, 16, 16), z(1, 1, 16, 16), z(1, 1, dtype=I32), z(2, dtype=I32), z(1, dtype=I32), **kw)
