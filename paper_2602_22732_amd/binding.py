@@ -496,6 +496,8 @@ def op_paged_attention(q, k_pages, v_pages, page_table, q_start, seq_len, k_new=
     if workspace is None:
         need = L.gr4ad_op_paged_attention_workspace_bytes(dt, cache, B, N, H, window, sinks)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    elif not workspace.is_contiguous():
+        raise ValueError("%s: workspace must be dense, got %s strides %s" % (what, tuple(workspace.shape), workspace.stride()))
     _check(L.gr4ad_op_paged_attention(dt, cache, q.data_ptr(), strides[0], _ptr(k_new), _ptr(v_new), strides[1] or 0, q_start.data_ptr(), seq_len.data_ptr(), out.data_ptr(), B, N, H,
                                       dh ** -0.5 if scale is None else scale, window, sinks, _ptr(workspace),
                                       0 if workspace is None else workspace.numel() * workspace.element_size(), _raw_stream(_device())))

@@ -47,3 +47,10 @@ def test_windows_that_32_bits_do_not_hold(anywhere, kw):
     z = anywhere
     with pytest.raises(ValueError, match="window"):
         binding.op_paged_attention(z(1, 2, 16), z(1, 1, 16, 16), z(1, 1, 16, 16), z(1, 1, dtype=I32), z(2, dtype=I32), z(1, dtype=I32), **kw)
+
+
+def test_workspace_must_be_dense(anywhere):
+    z = anywhere
+    for workspace in (z(2, 1 << 20, dtype=U8)[:, ::2], z(1, dtype=U8).expand(1 << 24)):
+        with pytest.raises(ValueError, match="workspace"):
+            binding.op_paged_attention(z(1, 2, 64), z(9, 1, 16, 64), z(9, 1, 64, 16), z(1, 4096, dtype=I32), z(2, dtype=I32), z(1, dtype=I32), workspace=workspace)
