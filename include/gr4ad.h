@@ -294,6 +294,7 @@ int gr4ad_op_gather_rows(gr4ad_dtype dtype, const void *src_dev, const int32_t *
  *                  max_pages * page_size (clamped).  Tokens at negative positions (seq_len[b] < m_b) are neither written nor see anything
  *   out            [N, H, dh] dtype, dense
  *   workspace_dev  gr4ad_op_paged_attention_workspace_bytes bytes of scratch (0: none), not shared by calls that overlap in time
+ * out, the workspace and pages that receive new tokens share no byte with any other buffer of the call (EINVAL).
  * float32 sums, maxima and normalisers; in bf16, long chunks round the softmax's weights once, as operands of the product with the values, and other
  * rows enter them as two bf16 numbers.  Same bits from run to run; a row's bits may depend on the batch it is in (which decides how its keys are split).
  * B, N >= 1; head widths 16, 32, 64, 128; page_size a power of two from 16 to 1024; q, k_new and v_new with their rows, out, both page arrays and the

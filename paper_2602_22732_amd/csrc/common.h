@@ -140,6 +140,19 @@ __device__ __forceinline__ int wave_scan(int x) {
 
 static inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Where an operand lies, in bytes: rows of `width`, `stride` apart (a NULL pointer or a width of 0: nowhere).
+struct Span {
+    const void *at;
+    int64_t width, rows = 1, stride = 0;
+};
+// whether a dense span shares a byte with a span of rows
+static inline bool overlap(const Span &dense, const Span &s) {
+    if (!dense.at || !s.at || dense.width <= 0 || s.width <= 0) return false;
+    const int64_t from = (int64_t)((uintptr_t)dense.at - (uintptr_t)s.at), to = from + dense.width;  // counted from s's first row
+    const int64_t first = from < s.width ? 0 : s.rows > 1 ? (from - s.width) / s.stride + 1 : 1;      // first row that ends behind `from`
+    return first < s.rows && first * s.stride < to;
+}
+
 // Records the message gr4ad_last_error(NULL) returns on this thread (entry points that take no decoder); returns `code`.
 int gr4ad_set_thread_error(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 

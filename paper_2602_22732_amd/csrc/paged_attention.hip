@@ -1273,10 +1273,17 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
     const Plan p = plan_of(dtype, B, N, H, c.H_kv, c.dh, c.page_size, c.max_pages, window, sinks);
     if (p.bytes && (!workspace || workspace_bytes < p.bytes || (uintptr_t)workspace % 16))
         return gr4ad_set_thread_error(GR4AD_EWORKSPACE, "paged attention: workspace of %zu bytes needed, 16-byte aligned", p.bytes);
+    const int e = dtype == GR4AD_BF16 ? 2 : 4;
+    // What is written shares no byte with anything else of the call (without new tokens the pages are only read).
+    const int64_t page_bytes = (int64_t)c.H_kv * c.page_size * c.dh * e, pages = page_bytes > INT64_MAX / 4 / c.n_pages ? INT64_MAX / 4 : page_bytes * c.n_pages, new_width = k_new ? (int64_t)c.H_kv * c.dh * e : 0;
+    const Span all[] = {{out, (int64_t)N * H * c.dh * e}, {workspace, (int64_t)p.bytes}, {c.k_pages, pages}, {c.v_pages, pages}, {q, (int64_t)H * c.dh * e, N, q_stride * e},
+                        {k_new, new_width, N, kv_stride * e}, {v_new, new_width, N, kv_stride * e}, {c.page_table, (int64_t)B * c.max_pages * 4}, {q_start, (B + 1LL) * 4}, {seq_len, B * 4LL}};
+    for (int i = 0; i < (k_new ? 4 : 2); i++)
+        for (size_t j = i + 1; j < sizeof(all) / sizeof(all[0]); j++)
+            if (overlap(all[i], all[j])) return gr4ad_set_thread_error(GR4AD_EINVAL, "paged attention: %s overlaps another buffer of the call", i == 0 ? "out" : i == 1 ? "the workspace" : "a page array");
     hipStream_t st = (hipStream_t)hip_stream;
     PagedArgs a = {q, q_stride, k_new, v_new, kv_stride, q_start, seq_len, c.page_table, c.k_pages, c.v_pages, c.n_pages, shift_of(c.page_size), c.max_pages, B, N, H, c.H_kv,
                    H / c.H_kv, scale * 1.4426950408889634f, window > kMostKeys ? kMostKeys : window, sinks > kMostKeys ? kMostKeys : sinks, out, (float *)workspace, p.nsplit};
-    const int e = dtype == GR4AD_BF16 ? 2 : 4;
     if (k_new && p.flash()) {  // (the smaller tiles take the new tokens where they are)
         int64_t tiles = (int64_t)N / kAppendKeys + 2 * (int64_t)B;
         if (tiles > N) tiles = N;

@@ -54,3 +54,42 @@ def test_workspace_must_be_dense(anywhere):
     for workspace in (z(2, 1 << 20, dtype=U8)[:, ::2], z(1, dtype=U8).expand(1 << 24)):
         with pytest.raises(ValueError, match="workspace"):
             binding.op_paged_attention(z(1, 2, 64), z(9, 1, 16, 64), z(9, 1, 64, 16), z(1, 4096, dtype=I32), z(2, dtype=I32), z(1, dtype=I32), workspace=workspace)
+
+
+K, M = 1 << 10, 1 << 20
+# an attention call whose buffers lie 16 MB apart: bf16, 2 rows of 4 heads of 64 columns, 3 pages of 16 positions of 2 key heads
+APART = dict(k=16 * M, v=32 * M, table=48 * M, q=64 * M, k_new=80 * M, v_new=96 * M, start=112 * M, len=128 * M, out=144 * M, ws=160 * M, q_stride=256, kv_stride=128, max_pages=4, n_pages=3, N=2)
+
+
+def attention(**over):
+    a = dict(APART, **over)
+    cache = binding.PagedCacheDesc(a["k"], a["v"], a["table"], a["n_pages"], 16, a["max_pages"], 2, 64)
+    return binding.lib().gr4ad_op_paged_attention(1, C.byref(cache), a["q"], a["q_stride"], a["k_new"], a["v_new"], a["kv_stride"], a["start"], a["len"], a["out"], 1, a["N"], 4, 0.1, 0, 0, a["ws"],
+                                                  1 << 22, None)
+
+
+ROW, PAGES = 4 * 64 * 2, 3 * 2 * 16 * 64 * 2  # bytes of a row of q, of an array of pages
+
+
+@pytest.mark.parametrize("over", [
+    dict(out=APART["q"]), dict(out=APART["q"] + 2 * ROW - 16), dict(out=APART["q"] - 2 * ROW + 16), dict(out=APART["q"] + 8 * K - 2 * ROW + 16, q_stride=4 * K), dict(out=APART["k_new"] + 16),
+    dict(out=APART["v_new"] + 496), dict(out=APART["k"] + PAGES - 16), dict(out=APART["v"]), dict(v=APART["k"] + PAGES - 16), dict(out=APART["table"] - 16), dict(start=APART["out"] + 1000),
+    dict(len=APART["out"]), dict(q=APART["v"] + 256), dict(k_new=APART["k"]), dict(max_pages=4096, ws=APART["q"] - 4 * K), dict(max_pages=4096, ws=APART["out"]), dict(max_pages=4096, ws=APART["k"] + 256),
+    dict(table=APART["k"] + 16),
+])
+def test_attention_buffers_that_overlap(over):
+    assert attention(**over) == -1
+    assert b"overlap" in binding.lib().gr4ad_last_error(None)
+
+
+def no_gpu():
+    """Calls that no check refuses: only where no launch can follow."""
+    if torch.cuda.is_available():
+        pytest.skip("with a GPU these would launch on addresses that are none")
+
+
+@pytest.mark.parametrize("over", [dict(out=APART["q"] + 2 * ROW), dict(out=APART["q"] - 2 * ROW), dict(out=APART["q"] + ROW, q_stride=4 * K), dict(out=APART["k"] + PAGES), dict(v=APART["k"] + PAGES),
+                                  dict(ws=APART["q"]), dict(k_new=None, v_new=None, q=APART["v"] + 256), dict(v_new=APART["k_new"])])
+def test_attention_buffers_side_by_side(over):
+    no_gpu()
+    assert attention(**over) == -4  # (as far as the launch)
