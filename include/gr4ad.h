@@ -337,7 +337,7 @@ int gr4ad_op_linear_fp8_block(const void *Aq_dev, const float *a_scale_dev, cons
  * times token v occurs in the row's history, in float32 and in this order:
  *   l = c > 0 ? (l > 0 ? l / repetition : l * repetition) : l;   l -= frequency * c + (c > 0 ? presence : 0);   l += bias[bias_row, v];
  *   l = -inf where the row's mask forbids v (whatever the logit holds).
- * logits, out [rows, V] float32 (_f16: IEEE half, rounded once), out may be logits itself.  rows >= 1, V from 1 to 2^30.  Every rule is optional (NULL).
+ * logits, out [rows, V] float32 (_f16: IEEE half, rounded once); out is logits itself or shares no byte with any other buffer (EINVAL).  rows >= 1, V from 1 to 2^30.  Every rule is optional (NULL).
  * The struct is host memory, its pointers device memory.
  */
 typedef struct {

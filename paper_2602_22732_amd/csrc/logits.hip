@@ -131,6 +131,13 @@ template <typename T> int adjust(const T *in, T *out, int32_t rows, int32_t V, c
     const int64_t stretches = ceil_div64(V, span), grid = rows * stretches;
     if (grid > 0x7fffffffLL || V > (1 << 30)) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "adjust_logits: %d rows of %d logits", rows, V);
     const int keep = (int64_t)rows * V * (int)sizeof(T) < (16 << 20) || V * sizeof(T) % 16 || (uintptr_t)out % 16;
+    // (a thread writes only what it has read itself where out is the logits' place, and reads the tables while others write)
+    const int64_t bytes = (int64_t)rows * V * (int64_t)sizeof(T), table = (int64_t)V * 4, words = ceil_div64(V, 32) * 4;
+    const Span o = {out, bytes}, others[] = {{(const void *)in == (const void *)out ? nullptr : in, bytes}, {r->history, r->history_stride * 4LL, rows, r->history_stride * 4LL},
+                                             {r->bias, table * r->n_bias}, {r->mask, words * r->n_masks}, {r->history_len, rows * 4LL}, {r->repetition, rows * 4LL}, {r->presence, rows * 4LL},
+                                             {r->frequency, rows * 4LL}, {r->bias_row, rows * 4LL}, {r->mask_row, rows * 4LL}};
+    for (const Span &s : others)
+        if (overlap(o, s)) return gr4ad_set_thread_error(GR4AD_EINVAL, "adjust_logits: out overlaps another buffer of the call and is not logits itself");
     hipStream_t st = (hipStream_t)stream;
     ProfScope ps(KC_ADJUST_LOGITS, st, 0.0, 2.0 * sizeof(T) * rows * (double)V);
     LogitArgs a = {in, out, rows, V, *r};

@@ -82,6 +82,16 @@ def test_attention_buffers_that_overlap(over):
     assert b"overlap" in binding.lib().gr4ad_last_error(None)
 
 
+@pytest.mark.parametrize("itemsize,entry", [(4, "gr4ad_op_adjust_logits"), (2, "gr4ad_op_adjust_logits_f16")])
+def test_logits_that_overlap(itemsize, entry):
+    rows, V, n = 3, 100, 300 * itemsize
+    f = getattr(binding.lib(), entry)
+    rules = binding.LogitRules(history=M, history_stride=5, bias=2 * M, n_bias=2, mask=3 * M, n_masks=2)
+    for logits, out in ((8 * M, 8 * M + itemsize), (8 * M, 8 * M - n + itemsize), (8 * M, M), (8 * M, M + 56), (8 * M, 2 * M + 796), (8 * M, 3 * M + 28)):
+        assert f(logits, out, rows, V, C.byref(rules), None) == -1
+        assert b"overlap" in binding.lib().gr4ad_last_error(None)
+
+
 def no_gpu():
     """Calls that no check refuses: only where no launch can follow."""
     if torch.cuda.is_available():
@@ -93,3 +103,9 @@ def no_gpu():
 def test_attention_buffers_side_by_side(over):
     no_gpu()
     assert attention(**over) == -4  # (as far as the launch)
+
+
+def test_logits_side_by_side():
+    no_gpu()
+    for logits, out in ((8 * M, 8 * M), (8 * M, 8 * M + 1200), (8 * M, 8 * M - 1200)):
+        assert binding.lib().gr4ad_op_adjust_logits(logits, out, 3, 100, C.byref(binding.LogitRules()), None) == -4
