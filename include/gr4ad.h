@@ -297,7 +297,7 @@ int gr4ad_op_gather_rows(gr4ad_dtype dtype, const void *src_dev, const int32_t *
  * out, the workspace and pages that receive new tokens share no byte with any other buffer of the call (EINVAL).
  * float32 sums, maxima and normalisers; in bf16, long chunks round the softmax's weights once, as operands of the product with the values, and other
  * rows enter them as two bf16 numbers.  Same bits from run to run; a row's bits may depend on the batch it is in (which decides how its keys are split).
- * B, N >= 1; head widths 16, 32, 64, 128; page_size a power of two from 16 to 1024; q, k_new and v_new with their rows, out, both page arrays and the
+ * B, N >= 1; max_pages * page_size, N * H and B * H_kv at most 2^30, H * dh below 2^31; head widths 16, 32, 64, 128; page_size a power of two from 16 to 1024; q, k_new and v_new with their rows, out, both page arrays and the
  * workspace 16-byte aligned.
  */
 typedef struct {

@@ -1245,6 +1245,8 @@ int check_shape(gr4ad_dtype dtype, const gr4ad_paged_cache *c, int32_t B, int32_
         return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: page_size %d is not a power of two from 16 to 1024", c->page_size);
     if ((int64_t)c->max_pages * c->page_size > kMostKeys || (int64_t)N * H > kMostKeys || (int64_t)B * c->H_kv > kMostKeys)
         return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: more than 2^30 positions of a sequence, rows times heads or sequences times heads");
+    if ((int64_t)H * c->dh > 0x7fffffffLL)  // (a column's place in its row is a number of 32 bits)
+        return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: rows of 2^31 values or more (%d heads of %d)", H, c->dh);
     return GR4AD_OK;
 }
 

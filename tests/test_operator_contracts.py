@@ -109,3 +109,19 @@ def test_logits_side_by_side():
     no_gpu()
     for logits, out in ((8 * M, 8 * M), (8 * M, 8 * M + 1200), (8 * M, 8 * M - 1200)):
         assert binding.lib().gr4ad_op_adjust_logits(logits, out, 3, 100, C.byref(binding.LogitRules()), None) == -4
+
+
+FAR = 1 << 42  # addresses whose buffers may have terabytes
+
+
+def wide_attention(N, H, H_kv, dh, dtype=1, B=1, new=False):
+    cache = binding.PagedCacheDesc(FAR, 2 * FAR, 3 * FAR, 2, 16, 1, H_kv, dh)
+    L, row = binding.lib(), H * dh
+    assert L.gr4ad_op_paged_attention_workspace_bytes(dtype, C.byref(cache), B, N, H, 0, 0) == 0
+    return L.gr4ad_op_paged_attention(dtype, C.byref(cache), 4 * FAR, row, 5 * FAR if new else None, 6 * FAR if new else None, H_kv * dh, 7 * FAR, 8 * FAR, 9 * FAR, B, N, H, 0.1, 0, 0, None, 0, None)
+
+
+@pytest.mark.parametrize("H,H_kv,dh", [(1 << 24, 1, 128), (1 << 27, 1 << 26, 16), (1 << 30, 1, 64)])
+def test_rows_of_2_to_the_31_values(H, H_kv, dh):
+    assert wide_attention(1, H, H_kv, dh) == -2
+    assert b"2^31" in binding.lib().gr4ad_last_error(None)
