@@ -297,7 +297,8 @@ int gr4ad_op_gather_rows(gr4ad_dtype dtype, const void *src_dev, const int32_t *
  * out, the workspace and pages that receive new tokens share no byte with any other buffer of the call (EINVAL).
  * float32 sums, maxima and normalisers; in bf16, long chunks round the softmax's weights once, as operands of the product with the values, and other
  * rows enter them as two bf16 numbers.  Same bits from run to run; a row's bits may depend on the batch it is in (which decides how its keys are split).
- * B, N >= 1; max_pages * page_size, N * H and B * H_kv at most 2^30, H * dh below 2^31; head widths 16, 32, 64, 128; page_size a power of two from 16 to 1024; q, k_new and v_new with their rows, out, both page arrays and the
+ * B, N >= 1; max_pages * page_size, N * H and B * H_kv at most 2^30, H * dh below 2^31, and no more workgroups
+ * than one launch takes (N * H / 16 + B * H_kv up to 2^22 always fit); head widths 16, 32, 64, 128; page_size a power of two from 16 to 1024; q, k_new and v_new with their rows, out, both page arrays and the
  * workspace 16-byte aligned.
  */
 typedef struct {
@@ -317,7 +318,8 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
  *   scale = amax / 448 and q = nearest OCP E4M3 value (ties to even) of x * (448 / amax), amax the block's largest magnitude (float32 operations);
  *   a block with amax < 2^-100 becomes zeros with scale 1.  A NaN becomes the E4M3 NaN; of a block that holds an infinity nothing is defined but that it has NaNs.
  * x [rows, n] float32 or bf16, rows x_stride elements apart; q [rows, n] bytes; scale [ceil(n / 128), ceil(rows / block_rows)] float32: blocks along n
- * first, as the product reads them.  Any rows and n from 1 to 2^31 - 256; the last blocks may be partial.
+ * first, as the product reads them.  n from 1 to 2^31 - 256, ceil(rows / 16) * ceil(n / 256) or, with block_rows = 128, ceil(rows / 128) * ceil(n / 128) below 2^24
+ * (one launch); the last blocks may be partial.
  */
 int gr4ad_op_quantize_blocks(gr4ad_dtype dtype, const void *x_dev, int64_t x_stride, void *q_dev, float *scale_dev, int32_t rows, int32_t n, int32_t block_rows,
                              void *hip_stream);
@@ -327,7 +329,8 @@ int gr4ad_op_quantize_blocks(gr4ad_dtype dtype, const void *x_dev, int64_t x_str
  * on operands of gr4ad_op_quantize_blocks (Aq with block_rows = 1, Wq with block_rows = 128): a_scale [ceil(K/128), M], w_scale [ceil(K/128), ceil(N/128)],
  * bias [N] float32 or NULL.  Every block's product is scaled and added in float32.  C is bf16, or IEEE half with out_f16 != 0 (logits for
  * gr4ad_op_adjust_logits_f16 and gr4ad_op_select_f16): the matrix cores keep about 16 bits of an FP8 product's sum, so there is no float32 form.
- * Any M, N, K from 1 to 2^31 - 256; rows dense.
+ * M, N, K from 1 to 2^31 - 256, with N at most 2^27 - 16 or, beyond 64 rows, ceil(M / 128) * ceil(N / 128) at most 2^22 (one launch; larger ones are refused where
+ * they do not fit); rows dense.
  */
 int gr4ad_op_linear_fp8_block(const void *Aq_dev, const float *a_scale_dev, const void *Wq_dev, const float *w_scale_dev, const float *bias_dev, void *C_dev,
                               int32_t M, int32_t N, int32_t K, int32_t out_f16, void *hip_stream);
@@ -337,7 +340,8 @@ int gr4ad_op_linear_fp8_block(const void *Aq_dev, const float *a_scale_dev, cons
  * times token v occurs in the row's history, in float32 and in this order:
  *   l = c > 0 ? (l > 0 ? l / repetition : l * repetition) : l;   l -= frequency * c + (c > 0 ? presence : 0);   l += bias[bias_row, v];
  *   l = -inf where the row's mask forbids v (whatever the logit holds).
- * logits, out [rows, V] float32 (_f16: IEEE half, rounded once); out is logits itself or shares no byte with any other buffer (EINVAL).  rows >= 1, V from 1 to 2^30.  Every rule is optional (NULL).
+ * logits, out [rows, V] float32 (_f16: IEEE half, rounded once); out is logits itself or shares no byte with any other buffer (EINVAL).  rows >= 1, V from 1 to 2^30,
+ * rows * max(64, V / 4) below 2^32 (one launch).  Every rule is optional (NULL).
  * The struct is host memory, its pointers device memory.
  */
 typedef struct {

@@ -509,7 +509,7 @@ int launch_ring(const BlockGemm &g, hipStream_t st) {
     const bool ragged = g.K % 128, edge = g.M % kRing;
     const auto kernel = ragged ? (edge ? gemm_block_ring<true, true> : gemm_block_ring<true, false>) : (edge ? gemm_block_ring<false, true> : gemm_block_ring<false, false>);
     const int64_t tiles_m = ceil_div64(g.M, kRing), tiles_n = ceil_div64(g.N, kRing), grid = (tiles_m * tiles_n + 7) / 8 * 8;
-    if (grid > 0x3fffffffLL) return too_many_tiles(g);
+    if (!launchable(grid, 512)) return too_many_tiles(g);
     if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return GR4AD_EHIP;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(512), LDS, st, g, (int)tiles_m, (int)tiles_n);
     GR4AD_LAUNCH_CHECK();
@@ -615,7 +615,7 @@ template <int TM, int TN, int SLOTS, bool RAGGED> __global__ __launch_bounds__(2
 template <int TM, int TN, int SLOTS> int launch_stream(const BlockGemm &g, hipStream_t st) {
     constexpr int LDS = SLOTS * ((TM + TN) * 128 + 4 * (TM < 64 ? 64 : TM));
     const int64_t grid = ceil_div64(g.M, TM) * ceil_div64(g.N, TN);
-    if (grid > 0x7fffffffLL) return too_many_tiles(g);
+    if (!launchable(grid, 256)) return too_many_tiles(g);
     const auto kernel = g.K % 128 ? gemm_block_stream<TM, TN, SLOTS, true> : gemm_block_stream<TM, TN, SLOTS, false>;
     if (LDS > 65536 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return GR4AD_EHIP;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), LDS, st, g);
@@ -625,7 +625,7 @@ template <int TM, int TN, int SLOTS> int launch_stream(const BlockGemm &g, hipSt
 
 template <int TM, int TN> int launch_tile(const BlockGemm &g, hipStream_t st) {
     const int64_t grid = ceil_div64(g.M, TM) * ceil_div64(g.N, TN);
-    if (grid > 0x7fffffffLL) return too_many_tiles(g);
+    if (!launchable(grid, 256)) return too_many_tiles(g);
     hipLaunchKernelGGL((gemm_block_tile<TM, TN>), dim3((unsigned)grid), dim3(256), 0, st, g);
     GR4AD_LAUNCH_CHECK();
     return GR4AD_OK;
@@ -633,7 +633,8 @@ template <int TM, int TN> int launch_tile(const BlockGemm &g, hipStream_t st) {
 
 template <int MG> int launch_few(const BlockGemm &g, hipStream_t st) {
     // as many column groups per workgroup as leave 256 workgroups
-    const int groups = (g.N + 15) / 16;
+    const int groups = (g.N + 15) / 16, each = MG == 1 || groups < 512 ? 1 : groups < 1024 ? 2 : 4;
+    if (!launchable((groups + each - 1) / each, 512)) return too_many_tiles(g);
     if (MG > 1 && groups >= 1024) hipLaunchKernelGGL((gemm_block_few<MG, 4>), dim3((groups + 3) / 4), dim3(512), 0, st, g);
     else if (MG > 1 && groups >= 512) hipLaunchKernelGGL((gemm_block_few<MG, 2>), dim3((groups + 1) / 2), dim3(512), 0, st, g);
     else hipLaunchKernelGGL((gemm_block_few<MG, 1>), dim3(groups), dim3(512), 0, st, g);
@@ -674,7 +675,7 @@ int gr4ad_op_quantize_blocks(gr4ad_dtype dtype, const void *x, int64_t x_stride,
     const bool tall = block_rows == 128;
     const int64_t nb = ceil_div64(n, 128), bands = ceil_div64(rows, tall ? 128 : 16), steps = tall ? 1 : 2, wide = ceil_div64(nb, steps), grid = bands * wide;
     const int keep = (int64_t)rows * n < (8 << 20) || n % 8 || (uintptr_t)q % 8;
-    if (grid > 0x7fffffffLL || n > 0x7fffff00) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "quantize_blocks: %d rows of %d values", rows, n);
+    if (!launchable(grid, 256) || n > 0x7fffff00) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "quantize_blocks: %d rows of %d values", rows, n);
     hipStream_t st = (hipStream_t)hip_stream;
     ProfScope ps(KC_QUANTIZE_BLOCKS, st, 0.0, (double)rows * n * (e + 1));
 #define QUANTIZE_(T, TALL) hipLaunchKernelGGL((quantize_blocks<T, TALL>), dim3((unsigned)grid), dim3(256), 0, st, (const T *)x, x_stride, (uint8_t *)q, scale, rows, n, (int)wide, (int)bands, keep)

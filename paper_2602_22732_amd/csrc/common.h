@@ -140,6 +140,9 @@ __device__ __forceinline__ int wave_scan(int x) {
 
 static inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// What one launch takes: fewer than 2^31 workgroups and fewer than 2^32 threads.
+static inline bool launchable(int64_t workgroups, int threads) { return workgroups <= 0x7fffffffLL && workgroups * threads < (1LL << 32); }
+
 // Where an operand lies, in bytes: rows of `width`, `stride` apart (a NULL pointer or a width of 0: nowhere).
 struct Span {
     const void *at;

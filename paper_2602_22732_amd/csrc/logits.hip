@@ -129,7 +129,7 @@ template <typename T> int adjust(const T *in, T *out, int32_t rows, int32_t V, c
     constexpr int E = Piece<T>::N;
     const int each = one ? E : 2 * E, threads = V <= 64 * each ? 64 : V <= 128 * each ? 128 : 256, span = threads * each;
     const int64_t stretches = ceil_div64(V, span), grid = rows * stretches;
-    if (grid > 0x7fffffffLL || V > (1 << 30)) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "adjust_logits: %d rows of %d logits", rows, V);
+    if (!launchable(grid, threads) || V > (1 << 30)) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "adjust_logits: %d rows of %d logits", rows, V);
     const int keep = (int64_t)rows * V * (int)sizeof(T) < (16 << 20) || V * sizeof(T) % 16 || (uintptr_t)out % 16;
     // (a thread writes only what it has read itself where out is the logits' place, and reads the tables while others write)
     const int64_t bytes = (int64_t)rows * V * (int64_t)sizeof(T), table = (int64_t)V * 4, words = ceil_div64(V, 32) * 4;

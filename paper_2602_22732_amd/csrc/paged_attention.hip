@@ -1200,7 +1200,7 @@ template <int DH, int NW, int SLOTS> int launch_flash(const PagedArgs &a, unsign
 
 template <typename T, int DH> int launch_rows(const PagedArgs &a, const Plan &p, hipStream_t st) {
     const int64_t grid = p.tiles * a.Hkv * a.nsplit, joined = p.join_tiles * a.Hkv * kRows;
-    if (grid > 0x7fffffffLL || joined > 0x7fffffffLL) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: %d rows of %d heads", a.N, a.H);
+    if (!launchable(grid, p.rows == kFlashRows ? 512 : 256) || (a.nsplit > 1 && !launchable(joined, 256))) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: %d rows of %d heads", a.N, a.H);
     if (p.rows == 16) {
         hipLaunchKernelGGL((paged_rows<T, DH, 1>), dim3((unsigned)grid), dim3(256), 0, st, a);
     } else if (p.rows == 32) {
@@ -1290,7 +1290,7 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
         int64_t tiles = (int64_t)N / kAppendKeys + 2 * (int64_t)B;
         if (tiles > N) tiles = N;
         const int64_t grid = tiles * c.H_kv;
-        if (grid > 0x7fffffffLL) return GR4AD_EUNSUPPORTED;
+        if (!launchable(grid, 256)) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: %d new tokens in %d sequences of %d key heads", N, B, c.H_kv);
         ProfScope ps(KC_PAGED_APPEND, st, 0.0, 4.0 * N * c.H_kv * c.dh * e);
         // (tiles of many rows: bf16, widths from 32 on)
         if (c.dh == 32) hipLaunchKernelGGL((paged_append<bf16, 32>), dim3((unsigned)grid), dim3(256), 0, st, a);

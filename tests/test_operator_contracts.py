@@ -125,3 +125,42 @@ def wide_attention(N, H, H_kv, dh, dtype=1, B=1, new=False):
 def test_rows_of_2_to_the_31_values(H, H_kv, dh):
     assert wide_attention(1, H, H_kv, dh) == -2
     assert b"2^31" in binding.lib().gr4ad_last_error(None)
+
+
+# One launch takes fewer than 2^32 threads.  The first size that is too large, and one below it that is not.
+@pytest.mark.parametrize("rows,n,block_rows,fits", [((1 << 28) - 15, 1, 1, False), ((1 << 28) - 16, 256, 1, True), ((1 << 28) - 16, 257, 1, False), ((1 << 30) + 1, 257, 128, False), ((1 << 30) + 1, 128, 128, True)])
+def test_quantiser_launch(rows, n, block_rows, fits):
+    if fits:
+        no_gpu()
+    assert binding.lib().gr4ad_op_quantize_blocks(1, FAR, n, 2 * FAR, 3 * FAR, rows, n, block_rows, None) == (-4 if fits else -2)
+    assert fits or b"quantize_blocks" in binding.lib().gr4ad_last_error(None)
+
+
+@pytest.mark.parametrize("M,N,K,fits", [(1, (1 << 27) - 15, 1, False), (1, (1 << 27) - 16, 1, True), (17, (1 << 29) - 63, 1, False), (64, (1 << 29) - 64, 1, True), (1 << 20, (1 << 19) + 1, 16, False),
+                                        (1 << 20, (1 << 19) - 256, 16, True), (1 << 20, (1 << 18) + 1, 17, False), (1 << 20, (1 << 18) - 128, 17, True)])
+def test_product_launch(M, N, K, fits):
+    if fits:
+        no_gpu()
+    assert binding.lib().gr4ad_op_linear_fp8_block(FAR, 2 * FAR, 3 * FAR, 4 * FAR, None, 5 * FAR, M, N, K, 0, None) == (-4 if fits else -2)
+    assert fits or b"linear_fp8_block" in binding.lib().gr4ad_last_error(None)
+
+
+@pytest.mark.parametrize("rows,V,fits", [(1 << 26, 8, False), ((1 << 26) - 1, 8, True), (1 << 24, 4096, False), ((1 << 24) - 1, 4096, True)])
+def test_logits_launch(rows, V, fits):
+    if fits:
+        no_gpu()
+    assert binding.lib().gr4ad_op_adjust_logits_f16(FAR, 2 * FAR, rows, V, C.byref(binding.LogitRules()), None) == (-4 if fits else -2)
+    assert fits or b"adjust_logits" in binding.lib().gr4ad_last_error(None)
+
+
+@pytest.mark.parametrize("N,H,H_kv,dh,dtype,B,new,fits", [
+    (1 << 25, 16, 16, 16, 0, 1, False, False), (1 << 24, 16, 16, 16, 0, 1, False, True),    # tiles of 32 rows
+    (1 << 24, 16, 16, 16, 0, 1 << 24, False, False),                                         # of 16, a sequence each
+    (1 << 26, 16, 16, 64, 1, 1, False, True),                                                # of 256
+    (1 << 21, 1 << 8, 1 << 8, 32, 1, 1 << 14, False, True), (1 << 21, 1 << 8, 1 << 8, 32, 1, 1 << 14, True, False),  # of 128; with their pages' update, 2^16 tiles of 256 heads
+])
+def test_attention_launch(N, H, H_kv, dh, dtype, B, new, fits):
+    if fits:
+        no_gpu()
+    assert wide_attention(N, H, H_kv, dh, dtype, B, new) == (-4 if fits else -2)
+    assert fits or b"paged attention" in binding.lib().gr4ad_last_error(None)
