@@ -504,15 +504,22 @@ template <bool RAGGED, bool EDGE> __global__ __launch_bounds__(512, 2) void gemm
 
 int too_many_tiles(const BlockGemm &g) { return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "linear_fp8_block: sizes %d x %d x %d", g.M, g.N, g.K); }
 
+// More than 64 KB of LDS has to be asked for, on each device: every launch asks for its own.
+int allow_lds(const void *kernel, int bytes) {
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return e == hipSuccess ? GR4AD_OK : thread_hip_error("linear_fp8_block", e);
+}
+
 int launch_ring(const BlockGemm &g, hipStream_t st) {
     constexpr int LDS = 5 * kRing * 128;
     const bool ragged = g.K % 128, edge = g.M % kRing;
     const auto kernel = ragged ? (edge ? gemm_block_ring<true, true> : gemm_block_ring<true, false>) : (edge ? gemm_block_ring<false, true> : gemm_block_ring<false, false>);
     const int64_t tiles_m = ceil_div64(g.M, kRing), tiles_n = ceil_div64(g.N, kRing), grid = (tiles_m * tiles_n + 7) / 8 * 8;
     if (!launchable(grid, 512)) return too_many_tiles(g);
-    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return GR4AD_EHIP;
+    const int s = allow_lds((const void *)kernel, LDS);
+    if (s) return s;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(512), LDS, st, g, (int)tiles_m, (int)tiles_n);
-    GR4AD_LAUNCH_CHECK();
+    GR4AD_LAUNCH_CHECK_AS("linear_fp8_block");
     return GR4AD_OK;
 }
 
@@ -617,9 +624,12 @@ template <int TM, int TN, int SLOTS> int launch_stream(const BlockGemm &g, hipSt
     const int64_t grid = ceil_div64(g.M, TM) * ceil_div64(g.N, TN);
     if (!launchable(grid, 256)) return too_many_tiles(g);
     const auto kernel = g.K % 128 ? gemm_block_stream<TM, TN, SLOTS, true> : gemm_block_stream<TM, TN, SLOTS, false>;
-    if (LDS > 65536 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS) != hipSuccess) return GR4AD_EHIP;
+    if (LDS > 65536) {
+        const int s = allow_lds((const void *)kernel, LDS);
+        if (s) return s;
+    }
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(256), LDS, st, g);
-    GR4AD_LAUNCH_CHECK();
+    GR4AD_LAUNCH_CHECK_AS("linear_fp8_block");
     return GR4AD_OK;
 }
 
@@ -627,7 +637,7 @@ template <int TM, int TN> int launch_tile(const BlockGemm &g, hipStream_t st) {
     const int64_t grid = ceil_div64(g.M, TM) * ceil_div64(g.N, TN);
     if (!launchable(grid, 256)) return too_many_tiles(g);
     hipLaunchKernelGGL((gemm_block_tile<TM, TN>), dim3((unsigned)grid), dim3(256), 0, st, g);
-    GR4AD_LAUNCH_CHECK();
+    GR4AD_LAUNCH_CHECK_AS("linear_fp8_block");
     return GR4AD_OK;
 }
 
@@ -638,7 +648,7 @@ template <int MG> int launch_few(const BlockGemm &g, hipStream_t st) {
     if (MG > 1 && groups >= 1024) hipLaunchKernelGGL((gemm_block_few<MG, 4>), dim3((groups + 3) / 4), dim3(512), 0, st, g);
     else if (MG > 1 && groups >= 512) hipLaunchKernelGGL((gemm_block_few<MG, 2>), dim3((groups + 1) / 2), dim3(512), 0, st, g);
     else hipLaunchKernelGGL((gemm_block_few<MG, 1>), dim3(groups), dim3(512), 0, st, g);
-    GR4AD_LAUNCH_CHECK();
+    GR4AD_LAUNCH_CHECK_AS("linear_fp8_block");
     return GR4AD_OK;
 }
 
@@ -683,7 +693,7 @@ int gr4ad_op_quantize_blocks(gr4ad_dtype dtype, const void *x, int64_t x_stride,
     else if (tall) QUANTIZE_(float, true);
     else QUANTIZE_(float, false);
 #undef QUANTIZE_
-    GR4AD_LAUNCH_CHECK();
+    GR4AD_LAUNCH_CHECK_AS("quantize_blocks");
     return GR4AD_OK;
 }
 

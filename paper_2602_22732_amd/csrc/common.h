@@ -340,3 +340,12 @@ void prof_rows(const int32_t *count_dev, int64_t rows, hipStream_t st);
         hipError_t e_ = hipGetLastError();                     \
         if (e_ != hipSuccess) return GR4AD_EHIP;               \
     } while (0)
+// The same for entry points that take no decoder: the message names the operator and what HIP says.
+static inline int thread_hip_error(const char *what, hipError_t e) {
+    return gr4ad_set_thread_error(GR4AD_EHIP, "%s: %s (%s)", what, hipGetErrorName(e), hipGetErrorString(e));
+}
+#define GR4AD_LAUNCH_CHECK_AS(what)                                 \
+    do {                                                            \
+        hipError_t e_ = hipGetLastError();                          \
+        if (e_ != hipSuccess) return thread_hip_error(what, e_);    \
+    } while (0)

@@ -144,7 +144,7 @@ template <typename T> int adjust(const T *in, T *out, int32_t rows, int32_t V, c
     const size_t lds = r->history ? span * sizeof(unsigned) : 0;
     if (one) hipLaunchKernelGGL((adjust_logits<T, 1>), dim3((unsigned)grid), dim3(threads), lds, st, a, (int)stretches, keep);
     else hipLaunchKernelGGL((adjust_logits<T, 2>), dim3((unsigned)grid), dim3(threads), lds, st, a, (int)stretches, keep);
-    GR4AD_LAUNCH_CHECK();
+    GR4AD_LAUNCH_CHECK_AS("adjust_logits");
     return GR4AD_OK;
 }
 

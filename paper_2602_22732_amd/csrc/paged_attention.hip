@@ -1185,7 +1185,8 @@ Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, 
 
 // More than 64 KB of LDS has to be asked for, on each device: every launch asks for its own.
 int allow_lds(const void *kernel, int bytes) {
-    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess ? GR4AD_OK : GR4AD_EHIP;
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    return e == hipSuccess ? GR4AD_OK : thread_hip_error("paged attention", e);
 }
 
 template <int DH, int NW, int SLOTS> int launch_flash(const PagedArgs &a, unsigned grid, hipStream_t st) {
@@ -1213,11 +1214,11 @@ template <typename T, int DH> int launch_rows(const PagedArgs &a, const Plan &p,
         else if constexpr (DH > 32) s = launch_flash<DH, kFlashRows / 32, 4>(a, (unsigned)grid, st);
         if (s) return s;
     }
-    GR4AD_LAUNCH_CHECK();
+    GR4AD_LAUNCH_CHECK_AS("paged attention");
     if (a.nsplit > 1) {
         if (a.nsplit >= 16) hipLaunchKernelGGL((paged_join<T, DH, 4>), dim3((unsigned)joined), dim3(256), 0, st, a);
         else hipLaunchKernelGGL((paged_join<T, DH, 1>), dim3((unsigned)(joined / 4)), dim3(256), 0, st, a);
-        GR4AD_LAUNCH_CHECK();
+        GR4AD_LAUNCH_CHECK_AS("paged attention");
     }
     return GR4AD_OK;
 }
@@ -1296,7 +1297,7 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
         if (c.dh == 32) hipLaunchKernelGGL((paged_append<bf16, 32>), dim3((unsigned)grid), dim3(256), 0, st, a);
         else if (c.dh == 64) hipLaunchKernelGGL((paged_append<bf16, 64>), dim3((unsigned)grid), dim3(256), 0, st, a);
         else hipLaunchKernelGGL((paged_append<bf16, 128>), dim3((unsigned)grid), dim3(256), 0, st, a);
-        GR4AD_LAUNCH_CHECK();
+        GR4AD_LAUNCH_CHECK_AS("paged attention");
     }
     // lengths lie on the device: counted on all pages of every sequence, an upper bound
     const double keys = (double)c.max_pages * c.page_size;

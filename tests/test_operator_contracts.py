@@ -164,3 +164,19 @@ def test_attention_launch(N, H, H_kv, dh, dtype, B, new, fits):
         no_gpu()
     assert wide_attention(N, H, H_kv, dh, dtype, B, new) == (-4 if fits else -2)
     assert fits or b"paged attention" in binding.lib().gr4ad_last_error(None)
+
+
+def test_failing_launches_say_so():
+    # every kind of launch without a GPU: the message is this call's and not an older one's
+    no_gpu()
+    L, rules = binding.lib(), C.byref(binding.LogitRules())
+    calls = [("paged attention", lambda N=N, dh=dh, dtype=dtype, new=new: wide_attention(N, 16, 2, dh, dtype, 1, new)) for N, dh, dtype, new in ((1, 64, 0, False), (5, 32, 1, False), (10, 64, 1, True), (100, 128, 1, False), (2000, 64, 1, True))]
+    calls += [("quantize_blocks", lambda: L.gr4ad_op_quantize_blocks(1, FAR, 8, 2 * FAR, 3 * FAR, 4, 8, 1, None))]
+    calls += [("linear_fp8_block", lambda M=M, N=N, K=K: L.gr4ad_op_linear_fp8_block(FAR, 2 * FAR, 3 * FAR, 4 * FAR, None, 5 * FAR, M, N, K, 0, None))
+              for M, N, K in ((4, 64, 128), (40, 20000, 128), (300, 300, 128), (2000, 2000, 128), (8192, 8192, 128), (300, 300, 130), (8192, 8192, 130))]
+    calls += [("adjust_logits", lambda f=f: f(FAR, 2 * FAR, 3, 100, rules, None)) for f in (L.gr4ad_op_adjust_logits, L.gr4ad_op_adjust_logits_f16)]
+    for name, call in calls:
+        assert L.gr4ad_op_quantize_blocks(9, FAR, 8, FAR, FAR, 4, 8, 1, None) == -1 and b"dtype" in L.gr4ad_last_error(None)
+        assert call() == -4
+        said = L.gr4ad_last_error(None).decode()
+        assert name in said and "hip" in said.lower(), said
