@@ -415,7 +415,7 @@ def op_gather_rows(src, parent, k=None, row_elems=None, stream=None):
 
 # ---- an autoregressive step's operators: attention over pages, block-scaled FP8 products, logits in front of the selection
 # These check devices, types, shapes and strides before the library sees a pointer and launch on `stream` (default: the current one of the operands' device),
-# for which they also allocate what is theirs.  A short call is bound by this side, so the checks are written to cost little where they hold.
+# for which they also allocate what is theirs.  A call without rows (an idle step) returns its empty results.  A short call is bound by this side, so the checks are written to cost little where they hold.
 _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -488,6 +488,8 @@ def op_paged_attention(q, k_pages, v_pages, page_table, q_start, seq_len, k_new=
         _beyond(what, window=window, sinks=sinks)
     if k_new is not None and v_new is not None and strides[1] != strides[2]:
         raise ValueError("%s: rows of k_new and v_new lie %d and %d values apart" % (what, strides[1], strides[2]))
+    if N == 0:  # (an idle step)
+        return torch.empty_like(q) if out is None else out
     L = lib()
     cache = C.byref(PagedCacheDesc(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), n_pages, page, max_pages, H_kv, dh))
     dt = BF16 if dtype is torch.bfloat16 else F32
@@ -518,6 +520,8 @@ def op_quantize_blocks(x, block_rows=1, stream=None):
         _beyond("op_quantize_blocks", rows=rows, n=n)
     q = torch.empty(rows, n, dtype=torch.uint8, device=x.device)
     scale = torch.empty(-(-n // 128), -(-rows // block_rows), dtype=torch.float32, device=x.device)
+    if rows == 0:
+        return q, scale
     _check(lib().gr4ad_op_quantize_blocks(BF16 if dtype is torch.bfloat16 else F32, x.data_ptr(), x.stride(0) if rows > 1 else n, q.data_ptr(), scale.data_ptr(), rows, n, block_rows,
                                           _raw_stream(_device())))
     return q, scale
@@ -544,6 +548,8 @@ def op_linear_fp8_block(Aq, a_scale, Wq, w_scale, bias=None, out_dtype=torch.bfl
     _dense(what, "out", out, out_dtype, (M, N))
     if out is None:
         out = torch.empty(M, N, dtype=out_dtype, device=Aq.device)
+    if M == 0:
+        return out
     _check(lib().gr4ad_op_linear_fp8_block(Aq.data_ptr(), a_scale.data_ptr(), Wq.data_ptr(), w_scale.data_ptr(), _ptr(bias), out.data_ptr(), M, N, K,
                                            1 if out_dtype is torch.float16 else 0, _raw_stream(_device())))
     return out
@@ -605,6 +611,10 @@ def op_adjust_logits(logits, history=None, history_len=None, repetition=None, pr
         out = torch.empty_like(logits)
     else:
         _dense(what, "out", out, dtype, shape)
+    if rows == 0 and V > 0:
+        return out
+    if history is not None and rules.history_stride == 0:  # (a first step: no token has been seen, so no penalty falls)
+        rules.history = rules.history_len = rules.repetition = rules.presence = rules.frequency = None
     L = lib()
     _check((L.gr4ad_op_adjust_logits if dtype is f32 else L.gr4ad_op_adjust_logits_f16)(logits.data_ptr(), out.data_ptr(), rows, V, C.byref(rules), _raw_stream(_device())))
     return out

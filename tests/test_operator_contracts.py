@@ -180,3 +180,24 @@ def test_failing_launches_say_so():
         assert call() == -4
         said = L.gr4ad_last_error(None).decode()
         assert name in said and "hip" in said.lower(), said
+
+
+def test_calls_without_rows(anywhere):
+    # an idle step: nothing to do and nothing launched (there is no GPU behind these tensors)
+    z = anywhere
+    cache = (z(9, 2, 16, 64), z(9, 2, 64, 16), z(3, 4, dtype=I32), z(4, dtype=I32), z(3, dtype=I32))
+    none = z(0, 4, 64)
+    assert binding.op_paged_attention(none, *cache).shape == (0, 4, 64)
+    assert binding.op_paged_attention(none, *cache, k_new=z(0, 2, 64), v_new=z(0, 2, 64), out=none) is none
+    with pytest.raises(ValueError):
+        binding.op_paged_attention(none, *cache, k_new=z(0, 3, 64), v_new=z(0, 2, 64))
+    q, scale = binding.op_quantize_blocks(z(0, 300))
+    assert q.shape == (0, 300) and scale.shape == (3, 0)
+    assert binding.op_quantize_blocks(z(0, 300, dtype=torch.bfloat16), 128)[1].shape == (3, 0)
+    c = binding.op_linear_fp8_block(q, scale, z(50, 300, dtype=U8), z(3, 1), out_dtype=torch.float16)
+    assert c.shape == (0, 50) and c.dtype == torch.float16
+    logits = z(0, 100)
+    assert binding.op_adjust_logits(logits, history=z(0, 5, dtype=I32), repetition=z(0), bias=z(1, 100), out=logits) is logits
+    assert binding.op_adjust_logits(z(2, 0, 100)).shape == (2, 0, 100)
+    with pytest.raises(ValueError):
+        binding.op_adjust_logits(logits, history=z(1, 5, dtype=I32))
