@@ -373,7 +373,9 @@ int gr4ad_op_adjust_logits_f16(const void *logits_f16_dev, void *out_f16_dev, in
  * The valid context lengths live on the device, so launches that depend on
  * them (cross-attention, the context key/value projections) are counted on
  * the padded length S - an upper bound; a caller that knows the lengths
- * rescales by mean(len)/S, as bench.py does.
+ * rescales by mean(len)/S, as bench.py does.  Attention over pages counts the
+ * keys that a window leaves; without one its flops and bytes are 0, since a
+ * table of pages says nothing about the lengths.
  * reset != 0 forgets the records afterwards.  Not thread-safe.
  */
 int gr4ad_profile_enable(int on);
