@@ -656,19 +656,18 @@ template <int MG> int launch_few(const BlockGemm &g, hipStream_t st) {
 // 64 x 64 or 128 x 128 tiles and one of 256 x 256, so each size is left when it needs more rounds than the next (x 4096 x 4096, tiles of 64, 128, 256: 128 rows 15,
 // 35, 46 us; 1024 rows, two rounds of the smallest, 34, 36, 45; 2048 rows, one round of the middle ones, 65, 46, 47; 2816 rows 90, 74, 49; 4096 rows 125, 86, 60).
 int launch_block_gemm(const BlockGemm &g, hipStream_t st) {
-    ProfScope ps(KC_GEMM_F8_BLOCK, st, 2.0 * (double)g.M * g.N * g.K, ((double)g.M + g.N) * g.K + 2.0 * (double)g.M * g.N);
     // rows in pieces of 16 bytes (and a tile's rows within 32 bits of its first): direct loads to LDS
     const bool aligned = g.K % 16 == 0 && g.K < (1 << 23) && (uintptr_t)g.A % 16 == 0 && (uintptr_t)g.W % 16 == 0;
-    if (g.M <= 16) return launch_few<1>(g, st);
-    if (g.M <= 32) return launch_few<2>(g, st);
-    if (g.M <= 64) return launch_few<4>(g, st);
-    if (aligned) {
-        if (ceil_div64(g.M, 64) * ceil_div64(g.N, 64) <= 1024) return launch_stream<64, 64, 4>(g, st);
-        if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) <= 512) return launch_stream<128, 128, 2>(g, st);
-        return launch_ring(g, st);
+    const int64_t tiles64 = ceil_div64(g.M, 64) * ceil_div64(g.N, 64), tiles128 = ceil_div64(g.M, 128) * ceil_div64(g.N, 128);
+    const int cls = g.M <= 64 ? KC_GEMM_F8_FEW : !aligned ? KC_GEMM_F8_ANY : tiles64 <= 1024 ? KC_GEMM_F8_64 : tiles128 <= 512 ? KC_GEMM_F8_128 : KC_GEMM_F8_256;
+    ProfScope ps(cls, st, 2.0 * (double)g.M * g.N * g.K, ((double)g.M + g.N) * g.K + 2.0 * (double)g.M * g.N);
+    switch (cls) {
+        case KC_GEMM_F8_FEW: return g.M <= 16 ? launch_few<1>(g, st) : g.M <= 32 ? launch_few<2>(g, st) : launch_few<4>(g, st);
+        case KC_GEMM_F8_64: return launch_stream<64, 64, 4>(g, st);
+        case KC_GEMM_F8_128: return launch_stream<128, 128, 2>(g, st);
+        case KC_GEMM_F8_256: return launch_ring(g, st);
+        default: return tiles128 < 256 ? launch_tile<64, 64>(g, st) : launch_tile<128, 128>(g, st);
     }
-    if (ceil_div64(g.M, 128) * ceil_div64(g.N, 128) < 256) return launch_tile<64, 64>(g, st);
-    return launch_tile<128, 128>(g, st);
 }
 
 }  // namespace

@@ -323,7 +323,7 @@ bool select_takes_f16(int V);
 // ---- optional per-kernel event timing ----------------------------------------
 enum KernelClass { KC_GEMM_TILE = 0, KC_GEMM_SIMPLE, KC_XATTN_FLASH, KC_XATTN_SIMPLE, KC_SELF_STEP, KC_TRUNK_SELF,
                    KC_RMSNORM, KC_FUSE_GATE, KC_SELECT_ROWS, KC_SELECT_REQUEST, KC_GATHER, KC_BROADCAST, KC_V_TRANSPOSE, KC_GEMM_RING, KC_SOFTMAX, KC_GEMM_RING_F8, KC_QUANTIZE, KC_CONTEXT_ATTN, KC_DISTINCT,
-                   KC_PAGED_APPEND, KC_PAGED_ATTN, KC_QUANTIZE_BLOCKS, KC_GEMM_F8_BLOCK, KC_ADJUST_LOGITS, KC_COUNT };
+                   KC_PAGED_APPEND, KC_PAGED_ATTN, KC_PAGED_FLASH, KC_QUANTIZE_BLOCKS, KC_GEMM_F8_FEW, KC_GEMM_F8_64, KC_GEMM_F8_128, KC_GEMM_F8_256, KC_GEMM_F8_ANY, KC_ADJUST_LOGITS, KC_COUNT };
 // Declared around a kernel launch: records an event before and (on scope exit) after it when timing is on.
 struct ProfScope {
     ProfScope(int cls, hipStream_t st, double flops = 0.0, double bytes = 0.0);  // algorithmic work of the launch

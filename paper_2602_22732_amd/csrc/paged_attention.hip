@@ -1301,7 +1301,7 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
     }
     // Lengths lie on the device and a table may be far longer: counted are the keys that a window leaves, for the sequences' average of new tokens; without one nothing.
     const double table = (double)c.max_pages * c.page_size, per_row = fmin(table, (double)window + sinks), per_sequence = fmin(table, per_row + ceil((double)N / B) - 1.0);
-    ProfScope ps(KC_PAGED_ATTN, st, window ? 4.0 * N * per_row * H * c.dh : 0.0, window ? e * (2.0 * B * per_sequence * c.H_kv * c.dh + 2.0 * N * H * c.dh) : 0.0);
+    ProfScope ps(p.flash() ? KC_PAGED_FLASH : KC_PAGED_ATTN, st, window ? 4.0 * N * per_row * H * c.dh : 0.0, window ? e * (2.0 * B * per_sequence * c.H_kv * c.dh + 2.0 * N * H * c.dh) : 0.0);
     return dtype == GR4AD_BF16 ? launch_width<bf16>(a, c.dh, p, st) : launch_width<float>(a, c.dh, p, st);
 }
 

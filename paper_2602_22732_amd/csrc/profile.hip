@@ -22,7 +22,8 @@ const char *kNames[KC_COUNT] = {"gemm_bf16_tile", "gemm_simple", "cross_attn_fla
                                 "cross_attn_simple", "self_attn_step", "trunk_self_attn", "rmsnorm", "fuse_gate", "select_rows",
                                 "select_request", "gather_rows", "broadcast_rows", "v_transpose", "gemm_bf16_ring", "masked_softmax_rows",
                                 "gemm_fp8_ring", "quantize_rows", "context_attn_flash_bf16", "distinct_rows",
-                                "paged_append", "paged_attention", "quantize_blocks", "gemm_fp8_block", "adjust_logits"};
+                                "paged_append", "paged_attention", "paged_attention_staged", "quantize_blocks", "gemm_fp8_block_few", "gemm_fp8_block_64", "gemm_fp8_block_128",
+                                "gemm_fp8_block_256", "gemm_fp8_block_unaligned", "adjust_logits"};
 }  // namespace
 
 ProfScope::ProfScope(int cls, hipStream_t st, double flops, double bytes) : idx_(-1), st_(st) {
