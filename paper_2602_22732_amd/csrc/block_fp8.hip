@@ -530,7 +530,8 @@ int launch_ring(const BlockGemm &g, hipStream_t st) {
 // ---------------------------------------------------------------------------------------------------------------------
 template <int TM, int TN, int SLOTS, bool RAGGED> __global__ __launch_bounds__(256) void gemm_block_stream(BlockGemm g) {
     constexpr int WM = TM / 2, WN = TN / 2, GM = WM / 16, GN = WN / 16, LA = TM / 32, LW = TN / 32, LEAD = SLOTS - 1, LOADS = LA + LW + 1;
-    constexpr int SLOT = (TM + TN) * 128 + 4 * (TM < 64 ? 64 : TM);  // bytes: rows of A, rows of W, A's scales
+    static_assert(TM >= 64, "a wavefront's load of 64 scales stays in the tile's rows");
+    constexpr int SLOT = (TM + TN) * 128 + 4 * TM;  // bytes: rows of A, rows of W, A's scales
     extern __shared__ intx4 smem[];
     char *lds = (char *)smem;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, c = lane / 16;
@@ -543,7 +544,7 @@ template <int TM, int TN, int SLOTS, bool RAGGED> __global__ __launch_bounds__(2
     for (int j = 0; j < LA; j++) a_off[j] = (unsigned)min((wave * LA + j) * 8 + lane / 8, last_a) * (unsigned)g.K + (unsigned)(ch0 ^ (((wave * LA + j) & 1) * 4)) * 16;
 #pragma unroll
     for (int j = 0; j < LW; j++) w_off[j] = (unsigned)min((wave * LW + j) * 8 + lane / 8, last_w) * (unsigned)g.K + (unsigned)(ch0 ^ (((wave * LW + j) & 1) * 4)) * 16;
-    const int s_row = min((wave * 64) % (TM < 64 ? 64 : TM) + lane, last_a);  // (what several wavefronts load twice is the same)
+    const int s_row = min((wave * 64) % TM + lane, last_a);  // (what several wavefronts load twice is the same)
     auto dma16 = [&](const void *src, int at) {
         __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1))) *)src, (void __attribute__((address_space(3))) *)(lds + at), 16, 0, 0);
     };
@@ -562,7 +563,7 @@ template <int TM, int TN, int SLOTS, bool RAGGED> __global__ __launch_bounds__(2
         for (int j = 0; j < LA; j++) dma16(from(base_a, a_off[j], wave * LA + j), at + (wave * LA + j) * 1024);
 #pragma unroll
         for (int j = 0; j < LW; j++) dma16(from(base_w, w_off[j], wave * LW + j), at + TM * 128 + (wave * LW + j) * 1024);
-        dma4(g.sa + (int64_t)kb * g.M + m0 + s_row, at + (TM + TN) * 128 + (wave * 256) % (4 * (TM < 64 ? 64 : TM)));
+        dma4(g.sa + (int64_t)kb * g.M + m0 + s_row, at + (TM + TN) * 128 + (wave * 256) % (4 * TM));
     };
     typedef const __attribute__((address_space(3))) intx4 *LdsChunk;
     typedef const __attribute__((address_space(3))) float *LdsFloat;
@@ -620,7 +621,7 @@ template <int TM, int TN, int SLOTS, bool RAGGED> __global__ __launch_bounds__(2
 }
 
 template <int TM, int TN, int SLOTS> int launch_stream(const BlockGemm &g, hipStream_t st) {
-    constexpr int LDS = SLOTS * ((TM + TN) * 128 + 4 * (TM < 64 ? 64 : TM));
+    constexpr int LDS = SLOTS * ((TM + TN) * 128 + 4 * TM);
     const int64_t grid = ceil_div64(g.M, TM) * ceil_div64(g.N, TN);
     if (!launchable(grid, 256)) return too_many_tiles(g);
     const auto kernel = g.K % 128 ? gemm_block_stream<TM, TN, SLOTS, true> : gemm_block_stream<TM, TN, SLOTS, false>;
@@ -644,10 +645,13 @@ template <int TM, int TN> int launch_tile(const BlockGemm &g, hipStream_t st) {
 template <int MG> int launch_few(const BlockGemm &g, hipStream_t st) {
     // as many column groups per workgroup as leave 256 workgroups
     const int groups = (g.N + 15) / 16, each = MG == 1 || groups < 512 ? 1 : groups < 1024 ? 2 : 4;
-    if (!launchable((groups + each - 1) / each, 512)) return too_many_tiles(g);
-    if (MG > 1 && groups >= 1024) hipLaunchKernelGGL((gemm_block_few<MG, 4>), dim3((groups + 3) / 4), dim3(512), 0, st, g);
-    else if (MG > 1 && groups >= 512) hipLaunchKernelGGL((gemm_block_few<MG, 2>), dim3((groups + 1) / 2), dim3(512), 0, st, g);
-    else hipLaunchKernelGGL((gemm_block_few<MG, 1>), dim3(groups), dim3(512), 0, st, g);
+    const dim3 grid((groups + each - 1) / each);
+    if (!launchable(grid.x, 512)) return too_many_tiles(g);
+    if constexpr (MG > 1) {
+        if (each == 4) hipLaunchKernelGGL((gemm_block_few<MG, 4>), grid, dim3(512), 0, st, g);
+        if (each == 2) hipLaunchKernelGGL((gemm_block_few<MG, 2>), grid, dim3(512), 0, st, g);
+    }
+    if (each == 1) hipLaunchKernelGGL((gemm_block_few<MG, 1>), grid, dim3(512), 0, st, g);
     GR4AD_LAUNCH_CHECK_AS("linear_fp8_block");
     return GR4AD_OK;
 }

@@ -69,7 +69,7 @@ def test_products_over_many_blocks(profile, M, N, K, kind, out):
     want, mag = Ad @ Wd.t(), Ad.abs() @ Wd.abs().t()
     # a matrix instruction's sum of 128 products keeps a limited number of bits below the largest (2e-4 of the magnitudes covers it), the blocks' sum adds nb steps of float32, and the
     # result is rounded once.  A block left out, or scaled as another, changes a sum of terms of both signs by about its magnitudes / (11 nb), 7e-4 of
-    # them at nb = 131, and by several times that in some of the thousands of sums that are looked at.
+    # them at nb = 130, and by several times that in some of the thousands of sums that are looked at.
     tol = (2e-4 + nb * 2.0 ** -24) * mag + want.abs() * torch.finfo(out).eps / 2 * (1 + 2e-4) + 2.0 ** -24
     far = (C.cpu()[rows][:, cols].double() - want).abs() - tol
     assert (far <= 0).all(), float((far / mag).max())
