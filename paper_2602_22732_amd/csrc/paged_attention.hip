@@ -7,7 +7,7 @@
 // The cache: keys [page][H_kv][slot][dh], values transposed [page][H_kv][dh][slot], so that a page of one head is one stretch of memory
 // and both operands of the two products, S^T = K Q^T and O^T = V^T P^T, are read along their contraction in 16-byte pieces.
 //
-//  * paged_append<T, DH>    new keys and values into their pages (ahead of paged_flash; the others take them where they are).
+//  * paged_append<DH>       new keys and values into their pages (ahead of paged_flash; the others take them where they are).
 //  * paged_rows<T, DH, MR>  16 or 32 rows (token, head of the group) of one (sequence, key head) per workgroup, whose wavefronts walk
 //                           stretches of the keys of their own; operands go from memory to registers.
 //  * paged_flash<DH, ..>    128 or 256 rows per workgroup, keys and values staged in LDS (bf16).
@@ -106,10 +106,9 @@ __device__ __forceinline__ int page_of(const PagedArgs &a, int b, int key) { ret
 // New keys and values of 64 positions (counted from the sequence's first) and one key head.  Positions on a page number that does not exist are left out.
 // Both are read in 16-byte pieces; the values turn in LDS and leave in pieces of 8 positions (one by one where not all of them are new): written one by one
 // from their rows they took most of 51 us for 4048 tokens of 8 heads of 128 columns.
-template <typename T, int DH> __global__ __launch_bounds__(256) void paged_append(PagedArgs a) {
-    constexpr int P = 16 / sizeof(T), CH = DH / P;  // values of a piece, pieces of a row
-    typedef T Piece __attribute__((ext_vector_type(P)));
-    __shared__ T turn[kAppendKeys][DH + 2];
+template <int DH> __global__ __launch_bounds__(256) void paged_append(PagedArgs a) {
+    constexpr int P = 8, CH = DH / P;  // values of a piece, pieces of a row
+    __shared__ bf16 turn[kAppendKeys][DH + 2];
     Sequence s;
     const int64_t t = blockIdx.x / a.Hkv;
     const int h = blockIdx.x % a.Hkv;
@@ -123,8 +122,8 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void paged_appen
     for (int i = threadIdx.x; i < (k1 - k0) * CH; i += 256) {
         const int key = k0 + i / CH, c = i % CH * P, id = page_of(a, s.b, key);
         const int64_t src = (int64_t)(s.start + key - base) * a.kv_stride + h * DH + c;
-        const Piece k = *(const Piece *)((const T *)a.k_new + src), v = *(const Piece *)((const T *)a.v_new + src);
-        if (id >= 0 && id < a.n_pages) *(Piece *)((T *)a.k + (((int64_t)id * a.Hkv + h) * page + (key & (page - 1))) * DH + c) = k;
+        const bf16x8 k = *(const bf16x8 *)((const bf16 *)a.k_new + src), v = *(const bf16x8 *)((const bf16 *)a.v_new + src);
+        if (id >= 0 && id < a.n_pages) *(bf16x8 *)((bf16 *)a.k + (((int64_t)id * a.Hkv + h) * page + (key & (page - 1))) * DH + c) = k;
 #pragma unroll
         for (int e = 0; e < P; e++) turn[key - tile0][c + e] = v[e];
     }
@@ -135,12 +134,12 @@ template <typename T, int DH> __global__ __launch_bounds__(256) void paged_appen
         if (key + P <= k0 || key >= k1) continue;
         const int id = page_of(a, s.b, key);
         if (id < 0 || id >= a.n_pages) continue;
-        T *dst = (T *)a.v + (((int64_t)id * a.Hkv + h) * DH + c) * page + (key & (page - 1));
+        bf16 *dst = (bf16 *)a.v + (((int64_t)id * a.Hkv + h) * DH + c) * page + (key & (page - 1));
         if (key >= k0 && key + P <= k1) {
-            Piece v;
+            bf16x8 v;
 #pragma unroll
             for (int e = 0; e < P; e++) v[e] = turn[g + e][c];
-            *(Piece *)dst = v;
+            *(bf16x8 *)dst = v;
         } else {
 #pragma unroll
             for (int e = 0; e < P; e++)
@@ -688,7 +687,7 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
 // of the products that the mask leaves; the matrix cores are busy for 40 % of the cycles, the rest is the softmax's and the reads of LDS.
 // ---------------------------------------------------------------------------------------------------------------------
 template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) void paged_flash(PagedArgs a) {
-    constexpr int QB = 1, ROWS = NW * 32 * QB, KT = 64, KCH = DH / 8, HALF = KT * KCH, KSTEPS = DH / 16, MT = DH / 32, KI = HALF / 64 / NW, LEAD = SLOTS - 1;
+    constexpr int ROWS = NW * 32, KT = 64, KCH = DH / 8, HALF = KT * KCH, KSTEPS = DH / 16, MT = DH / 32, KI = HALF / 64 / NW, LEAD = SLOTS - 1;
     static_assert(KI * 64 * NW == HALF, "every wavefront loads as much of a tile");
     extern __shared__ bf16x8 smem[];  // keys of SLOTS tiles, values of SLOTS tiles: HALF chunks each
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), frow = lane % 32, hf = lane / 32;
@@ -701,17 +700,16 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
     const Blocks bl = visible_blocks<KT>(a, p_lo, p_hi);
     const int each = (bl.count + a.nsplit - 1) / a.nsplit, x0 = min(split * each, bl.count), x1 = min(x0 + each, bl.count);
 
-    const int W0 = R0 + wave * 32 * QB;  // the wavefront's first row
-    int p[QB];
-    bf16x8 qf[QB][KSTEPS];
-#pragma unroll
-    for (int i = 0; i < QB; i++) {
-        const int R = W0 + 32 * i + frow, tok = R / a.group, head = kvh * a.group + R - tok * a.group;
-        p[i] = R < R1 ? base + tok : -1;
+    const int W0 = R0 + wave * 32;  // the wavefront's first row
+    int p;
+    bf16x8 qf[KSTEPS];
+    {
+        const int R = W0 + frow, tok = R / a.group, head = kvh * a.group + R - tok * a.group;
+        p = R < R1 ? base + tok : -1;
         // (rows past the last repeat a token's: they are computed and dropped)
         const bf16 *q = (const bf16 *)a.q + (int64_t)(s.start + min(tok, s.m - 1)) * a.q_stride + head * DH + 8 * hf;
 #pragma unroll
-        for (int st = 0; st < KSTEPS; st++) qf[i][st] = *(const bf16x8 *)(q + 16 * st);
+        for (int st = 0; st < KSTEPS; st++) qf[st] = *(const bf16x8 *)(q + 16 * st);
     }
 
     // Page numbers: one of 64 successive pages per lane.  Every wavefront loads its share of a tile, so all keep them.
@@ -777,17 +775,12 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
         return (unsigned)__builtin_amdgcn_ballot_w64(exists(id)) & 0xFFu;
     };
 
-    float m_run[QB], l_run[QB];
-    floatx16 o[QB][MT];
+    float m_run = -INFINITY, l_run = 0.0f;
+    floatx16 o[MT];
 #pragma unroll
-    for (int i = 0; i < QB; i++) {
-        m_run[i] = -INFINITY;
-        l_run[i] = 0.0f;
+    for (int mt = 0; mt < MT; mt++)
 #pragma unroll
-        for (int mt = 0; mt < MT; mt++)
-#pragma unroll
-            for (int v = 0; v < 16; v++) o[i][mt][v] = 0.0f;
-    }
+        for (int v = 0; v < 16; v++) o[mt][v] = 0.0f;
     // Fragments by their LDS address: chunk c of row r lies at c ^ swizzle(r), and c = 2 step + hf, so a step flips bits above the lane's own address; the
     // address is made anew for every tile (kept for every step it costs registers that spill).
     typedef const __attribute__((address_space(3))) bf16x8 *LdsChunk;
@@ -801,29 +794,27 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
     };
     auto key_frag = [&](unsigned k, int sub, int st) { return *((LdsChunk)(k ^ (unsigned)(st << 5)) + sub * 32 * KCH); };
     auto value_frag = [&](unsigned v, int ks, int mt) { return *((LdsChunk)(v ^ (unsigned)(ks << 5)) + mt * 256); };
-    struct Scores { floatx16 s[QB][2]; };  // a lane holds, of its row, keys 32 sub + 16 (v / 8) + 8 hf + v % 8
-    bf16x8 pf[QB][4];  // weights, rounded once as the operand of the matrix instruction (the normaliser adds them unrounded)
-    float neg[QB];     // minus the maximum in use
-    // two weights of row i, keys 2 j and 2 j + 1 of the lane's 32, in two parts: the exponentials, and (a step later, when they are there) their sum and rounding
+    struct Scores { floatx16 s[2]; };  // a lane holds, of its row, keys 32 sub + 16 (v / 8) + 8 hf + v % 8
+    bf16x8 pf[4];  // weights, rounded once as the operand of the matrix instruction (the normaliser adds them unrounded)
+    float neg;     // minus the maximum in use
+    // two weights of the lane's row, keys 2 u and 2 u + 1 of its 32, in two parts: the exponentials, and (a step later, when they are there) their sum and rounding
     auto weigh = [&](Scores &c, int u) {
-        const int i = u % QB, k = 2 * (u / QB);
 #pragma unroll
-        for (int e = k; e < k + 2; e++) {
-            float w = __builtin_amdgcn_exp2f(__builtin_fmaf(c.s[i][e / 16][e % 16], a.scale_log2e, neg[i]));
+        for (int e = 2 * u; e < 2 * u + 2; e++) {
+            float w = __builtin_amdgcn_exp2f(__builtin_fmaf(c.s[e / 16][e % 16], a.scale_log2e, neg));
             asm volatile("" : "+v"(w));  // (formed here, beside the matrix instructions, and not in the later block that uses it)
-            c.s[i][e / 16][e % 16] = w;
+            c.s[e / 16][e % 16] = w;
         }
     };
     auto settle = [&](const Scores &c, int u) {
-        const int i = u % QB, k = 2 * (u / QB);
 #pragma unroll
-        for (int e = k; e < k + 2; e++) {
-            const float w = c.s[i][e / 16][e % 16];
-            l_run[i] += w;
-            pf[i][e / 8][e % 8] = (bf16)w;
+        for (int e = 2 * u; e < 2 * u + 2; e++) {
+            const float w = c.s[e / 16][e % 16];
+            l_run += w;
+            pf[e / 8][e % 8] = (bf16)w;
         }
-        asm volatile("" : "+v"(l_run[i]));
-        if (k % 8 == 6) asm volatile("" : "+v"(pf[i][k / 8]));
+        asm volatile("" : "+v"(l_run));
+        if (u % 4 == 3) asm volatile("" : "+v"(pf[u / 4]));
     };
     auto weights_upto = [&](Scores &c, int u0, int u1) {
 #pragma unroll
@@ -834,12 +825,12 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
     };
 #define SB __builtin_amdgcn_sched_barrier(0)
     constexpr int AHEAD = 4;
-    constexpr int PAIRS = 16 * QB, UNDER_SCORES = 12 * QB;  // pairs of weights of a tile; those formed under the next tile's first product
+    constexpr int PAIRS = 16, UNDER_SCORES = 12;  // pairs of weights of a tile; those formed under the next tile's first product
     // scores of a tile into n, beside the weights of the tile in c (WEIGH; without NEXT the weights alone).  The two halves of the keys in turn, so that the
     // weights have left half of c's registers before the second half of n needs its own.
     auto scores = [&](auto next, auto weights, unsigned sk, Scores &n, Scores &c) {
         constexpr bool NEXT = decltype(next)::value, WEIGH = decltype(weights)::value;
-        constexpr int MM = 2 * KSTEPS * QB;
+        constexpr int MM = 2 * KSTEPS;
         bf16x8 kf[AHEAD];  // fragments are read AHEAD - 1 steps before their MFMAs: the LDS answers in the time of several
         if constexpr (NEXT) {
 #pragma unroll
@@ -849,32 +840,25 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
         for (int sub = 0; sub < 2; sub++) {
             if constexpr (NEXT) {
 #pragma unroll
-                for (int i = 0; i < QB; i++)
-#pragma unroll
-                    for (int v = 0; v < 16; v++) n.s[i][sub][v] = 0.0f;
+                for (int v = 0; v < 16; v++) n.s[sub][v] = 0.0f;
             }
 #pragma unroll
             for (int st = 0; st < KSTEPS; st++) {
                 const int f = sub * KSTEPS + st, ahead = f + AHEAD - 1;
                 if constexpr (NEXT)
                     if (ahead < 2 * KSTEPS) kf[ahead % AHEAD] = key_frag(sk, ahead / KSTEPS, ahead % KSTEPS);
-#pragma unroll
-                for (int i = 0; i < QB; i++) {
-                    const int at = f * QB + i;
-                    if constexpr (NEXT) n.s[i][sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[f % AHEAD], qf[i][st], n.s[i][sub], 0, 0, 0);
-                    if constexpr (WEIGH) weights_upto(c, at * UNDER_SCORES / MM, (at + 1) * UNDER_SCORES / MM);
-                    SB;
-                }
+                if constexpr (NEXT) n.s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[f % AHEAD], qf[st], n.s[sub], 0, 0, 0);
+                if constexpr (WEIGH) weights_upto(c, f * UNDER_SCORES / MM, (f + 1) * UNDER_SCORES / MM);
+                SB;
             }
         }
     };
-    float mx[QB];
+    float mx;
     // values of a tile, beside its last weights and the maxima of the scores in n
     auto values = [&](auto next, unsigned sv, Scores &c, Scores &n) {
         constexpr bool NEXT = decltype(next)::value;
-        constexpr int MM = 4 * MT * QB, LATE = PAIRS - UNDER_SCORES;
-#pragma unroll
-        for (int i = 0; i < QB; i++) mx[i] = -INFINITY;
+        constexpr int MM = 4 * MT, LATE = PAIRS - UNDER_SCORES, half = MM / 2;
+        mx = -INFINITY;
         bf16x8 vf[AHEAD];
 #pragma unroll
         for (int g = 0; g < AHEAD - 1; g++) vf[g] = value_frag(sv, g / MT, g % MT);
@@ -884,22 +868,15 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
             for (int mt = 0; mt < MT; mt++) {
                 const int g = ks * MT + mt;
                 if (g + AHEAD - 1 < 4 * MT) vf[(g + AHEAD - 1) % AHEAD] = value_frag(sv, (g + AHEAD - 1) / MT, (g + AHEAD - 1) % MT);
+                o[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[g % AHEAD], pf[ks], o[mt], 0, 0, 0);
+                if (g < half) {
+                    weights_upto(c, UNDER_SCORES + g * LATE / half, UNDER_SCORES + (g + 1) * LATE / half);
+                    if (g == half - 1) settle(c, PAIRS - 1);
+                } else if constexpr (NEXT) {
 #pragma unroll
-                for (int i = 0; i < QB; i++) {
-                    const int at = g * QB + i, half = MM / 2;
-                    o[i][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[g % AHEAD], pf[i][ks], o[i][mt], 0, 0, 0);
-                    if (at < half) {
-                        weights_upto(c, UNDER_SCORES + at * LATE / half, UNDER_SCORES + (at + 1) * LATE / half);
-                        if (at == half - 1) settle(c, PAIRS - 1);
-                    } else if constexpr (NEXT) {
-#pragma unroll
-                        for (int u = (at - half) * PAIRS / half; u < (at - half + 1) * PAIRS / half; u++) {
-                            const int r = u % QB, k = 2 * (u / QB);
-                            mx[r] = fmaxf(fmaxf(mx[r], n.s[r][k / 16][k % 16]), n.s[r][k / 16][k % 16 + 1]);
-                        }
-                    }
-                    SB;
+                    for (int u = (g - half) * PAIRS / half; u < (g - half + 1) * PAIRS / half; u++) mx = fmaxf(fmaxf(mx, n.s[u / 8][2 * u % 16]), n.s[u / 8][2 * u % 16 + 1]);
                 }
+                SB;
             }
     };
     auto mask = [&](int key0, unsigned valid, Scores &n) {
@@ -908,48 +885,37 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
             asm volatile("" : "+v"(hf_));  // (nothing of this is kept in registers over the tiles that need none of it)
             const unsigned ok = valid >> hf_;
             const int k0 = key0 + 8 * hf_, sinks = a.window ? a.sinks - k0 : KT;
+            const int last = p - k0, from = a.window ? last - a.window + 1 : 0;  // of the lane's keys, counted from k0
 #pragma unroll
-            for (int i = 0; i < QB; i++) {
-                const int last = p[i] - k0, from = a.window ? last - a.window + 1 : 0;  // of the lane's keys, counted from k0
+            for (int sub = 0; sub < 2; sub++)
 #pragma unroll
-                for (int sub = 0; sub < 2; sub++)
-#pragma unroll
-                    for (int v = 0; v < 16; v++) {
-                        const int kk = 32 * sub + 16 * (v / 8) + v % 8;
-                        const bool seen = (kk <= last) & ((kk >= from) | (kk < sinks)) & ((ok >> (kk / 8) & 1) != 0);
-                        n.s[i][sub][v] = seen ? n.s[i][sub][v] : -INFINITY;
-                    }
-            }
+                for (int v = 0; v < 16; v++) {
+                    const int kk = 32 * sub + 16 * (v / 8) + v % 8;
+                    const bool seen = (kk <= last) & ((kk >= from) | (kk < sinks)) & ((ok >> (kk / 8) & 1) != 0);
+                    n.s[sub][v] = seen ? n.s[sub][v] : -INFINITY;
+                }
         }
     };
     auto follow = [&]() {  // the maximum in use follows when some row outgrew it by 2^8: terms up to 256 harm nothing
-        bool outgrown = false;
-#pragma unroll
-        for (int i = 0; i < QB; i++) {
-            mx[i] = halves_max(mx[i]) * a.scale_log2e;
-            outgrown |= mx[i] > m_run[i] + 8.0f;
-        }
+        mx = halves_max(mx) * a.scale_log2e;
+        const bool outgrown = mx > m_run + 8.0f;
         if (__builtin_amdgcn_ballot_w64(outgrown) != 0) {
             // In place by hand: as plain products the sums get second registers and a copy on the common path, 64 of them at DH = 128.  The matrix
             // instructions' results may be read after the pause (at most 19 wait states).
             asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+            const float mn = outgrown ? mx : m_run, alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - mn);
+            m_run = mn;
+            l_run *= alpha;
 #pragma unroll
-            for (int i = 0; i < QB; i++) {
-                const float mn = mx[i] > m_run[i] + 8.0f ? mx[i] : m_run[i], alpha = m_run[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[i] - mn);
-                m_run[i] = mn;
-                l_run[i] *= alpha;
+            for (int mt = 0; mt < MT; mt++)
 #pragma unroll
-                for (int mt = 0; mt < MT; mt++)
-#pragma unroll
-                    for (int v = 0; v < 16; v++) {
-                        float x = o[i][mt][v];
-                        asm volatile("v_mul_f32 %0, %0, %1" : "+v"(x) : "v"(alpha));
-                        o[i][mt][v] = x;
-                    }
-            }
+                for (int v = 0; v < 16; v++) {
+                    float x = o[mt][v];
+                    asm volatile("v_mul_f32 %0, %0, %1" : "+v"(x) : "v"(alpha));
+                    o[mt][v] = x;
+                }
         }
-#pragma unroll
-        for (int i = 0; i < QB; i++) neg[i] = m_run[i] == -INFINITY ? 0.0f : -m_run[i];
+        neg = m_run == -INFINITY ? 0.0f : -m_run;
     };
     // Group x of the loads: the values of tile x and the keys of tile x + 1, into slots x and x + 1 (modulo SLOTS).  Past the end the last tile is loaded again,
     // into slots that nobody reads any more, so that the waits need no cases.
@@ -989,12 +955,9 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
         meet(std::integral_constant<int, LEAD>());
         scores(yes, no, at_tile(k_lane, 0), s0, s1);
         mask(bl.at(x0) * KT, (unsigned)valid & 0xFF, s0);
+        mx = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < QB; i++) {
-            mx[i] = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < 32; k++) mx[i] = fmaxf(mx[i], s0.s[i][k / 16][k % 16]);
-        }
+        for (int k = 0; k < 32; k++) mx = fmaxf(mx, s0.s[k / 16][k % 16]);
         follow();
         int slot = 0;  // of tile x
         auto after = [&](int n) { return slot + n >= SLOTS ? slot + n - SLOTS : slot + n; };
@@ -1051,24 +1014,22 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
 #undef SB
     const PagedArgs z = late_args();
     bool bad = false;
-#pragma unroll
-    for (int i = 0; i < QB; i++) {
-        const float l = halves_sum(l_run[i]);
-        const int R = W0 + 32 * i + frow, tok = R / z.group, head = kvh * z.group + R - tok * z.group, row = s.start + tok;
-        if (R >= R1) continue;
+    const float l = halves_sum(l_run);
+    const int R = W0 + frow, tok = R / z.group, head = kvh * z.group + R - tok * z.group, row = s.start + tok;
+    if (R < R1) {
         bad |= !(l < INFINITY);
 #pragma unroll
         for (int mt = 0; mt < MT; mt++)
 #pragma unroll
-            for (int v = 0; v < 16; v++) bad |= !(fabsf(o[i][mt][v]) < INFINITY);
+            for (int v = 0; v < 16; v++) bad |= !(fabsf(o[mt][v]) < INFINITY);
         if (z.nsplit > 1) {
             float *part = part_row<DH>(z, row, head, split);
 #pragma unroll
             for (int mt = 0; mt < MT; mt++)
 #pragma unroll
-                for (int v = 0; v < 16; v++) part[mt * 32 + 8 * (v / 4) + 4 * hf + v % 4] = o[i][mt][v];
+                for (int v = 0; v < 16; v++) part[mt * 32 + 8 * (v / 4) + 4 * hf + v % 4] = o[mt][v];
             if (hf == 0) {
-                part[DH] = m_run[i];
+                part[DH] = m_run;
                 part[DH + 1] = l;
             }
         } else {
@@ -1080,13 +1041,13 @@ template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) vo
                 for (int g = 0; g < 4; g++) {
                     bf16x4 pk;
 #pragma unroll
-                    for (int j = 0; j < 4; j++) pk[j] = (bf16)(o[i][mt][4 * g + j] * inv);
+                    for (int j = 0; j < 4; j++) pk[j] = (bf16)(o[mt][4 * g + j] * inv);
                     *(bf16x4 *)(dst + mt * 32 + 8 * g + 4 * hf) = pk;
                 }
         }
     }
     if (__builtin_amdgcn_ballot_w64(bad) != 0)
-        for (int r = W0; r < W0 + 32 * QB && r < R1; r++) {
+        for (int r = W0; r < W0 + 32 && r < R1; r++) {
             const int tk = r / z.group;
             plain_row<bf16, DH, KT>(z, s, bl, x0, x1, kvh, s.start + tk, kvh * z.group + r - tk * z.group, base + tk, split);
         }
@@ -1294,9 +1255,9 @@ int gr4ad_op_paged_attention(gr4ad_dtype dtype, const gr4ad_paged_cache *cache, 
         if (!launchable(grid, 256)) return gr4ad_set_thread_error(GR4AD_EUNSUPPORTED, "paged attention: %d new tokens in %d sequences of %d key heads", N, B, c.H_kv);
         ProfScope ps(KC_PAGED_APPEND, st, 0.0, 4.0 * N * c.H_kv * c.dh * e);
         // (tiles of many rows: bf16, widths from 32 on)
-        if (c.dh == 32) hipLaunchKernelGGL((paged_append<bf16, 32>), dim3((unsigned)grid), dim3(256), 0, st, a);
-        else if (c.dh == 64) hipLaunchKernelGGL((paged_append<bf16, 64>), dim3((unsigned)grid), dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((paged_append<bf16, 128>), dim3((unsigned)grid), dim3(256), 0, st, a);
+        if (c.dh == 32) hipLaunchKernelGGL((paged_append<32>), dim3((unsigned)grid), dim3(256), 0, st, a);
+        else if (c.dh == 64) hipLaunchKernelGGL((paged_append<64>), dim3((unsigned)grid), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((paged_append<128>), dim3((unsigned)grid), dim3(256), 0, st, a);
         GR4AD_LAUNCH_CHECK_AS("paged attention");
     }
     // Lengths lie on the device and a table may be far longer: counted are the keys that a window leaves, for the sequences' average of new tokens; without one nothing.
