@@ -571,24 +571,23 @@ def op_adjust_logits(logits, history=None, history_len=None, repetition=None, pr
     V = shape[-1]
     rows = logits.numel() // V if V else 0
     one = (rows,)
-    if (rows | V) >> 31:
-        _beyond(what, rows=rows, V=V)
     rules = LogitRules()
+    most = n_bias = n_masks = 0
     if history is not None:
-        _dense(what, "history", history, i32, (rows, history.shape[-1]))
-        if history.shape[1] >> 31:
-            _beyond(what, history=history.shape[1])
-        rules.history, rules.history_stride = history.data_ptr(), history.shape[1]
+        most = history.shape[-1]
+        _dense(what, "history", history, i32, (rows, most))
+        rules.history = history.data_ptr()
     if bias is not None:
-        _dense(what, "bias", bias, f32, (bias.shape[0], V))
-        if bias.shape[0] >> 31:
-            _beyond(what, bias=bias.shape[0])
-        rules.bias, rules.n_bias = bias.data_ptr(), bias.shape[0]
+        n_bias = bias.shape[0]
+        _dense(what, "bias", bias, f32, (n_bias, V))
+        rules.bias = bias.data_ptr()
     if mask is not None:
-        _dense(what, "mask", mask, i32, (mask.shape[0], -(-V // 32)))
-        if mask.shape[0] >> 31:
-            _beyond(what, mask=mask.shape[0])
-        rules.mask, rules.n_masks = mask.data_ptr(), mask.shape[0]
+        n_masks = mask.shape[0]
+        _dense(what, "mask", mask, i32, (n_masks, -(-V // 32)))
+        rules.mask = mask.data_ptr()
+    if (rows | V | most | n_bias | n_masks) >> 31:
+        _beyond(what, rows=rows, V=V, history=most, bias=n_bias, mask=n_masks)
+    rules.history_stride, rules.n_bias, rules.n_masks = most, n_bias, n_masks
     if history_len is not None:
         _dense(what, "history_len", history_len, i32, one)
         rules.history_len = history_len.data_ptr()
@@ -613,7 +612,7 @@ def op_adjust_logits(logits, history=None, history_len=None, repetition=None, pr
         _dense(what, "out", out, dtype, shape)
     if rows == 0 and V > 0:
         return out
-    if history is not None and rules.history_stride == 0:  # (a first step: no token has been seen, so no penalty falls)
+    if most == 0 and history is not None:  # (a first step: no token has been seen, so no penalty falls)
         rules.history = rules.history_len = rules.repetition = rules.presence = rules.frequency = None
     L = lib()
     _check((L.gr4ad_op_adjust_logits if dtype is f32 else L.gr4ad_op_adjust_logits_f16)(logits.data_ptr(), out.data_ptr(), rows, V, C.byref(rules), _raw_stream(_device())))
