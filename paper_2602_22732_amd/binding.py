@@ -587,6 +587,8 @@ def op_adjust_logits(logits, history=None, history_len=None, repetition=None, pr
         rules.mask = mask.data_ptr()
     if (rows | V | most | n_bias | n_masks) >> 31:
         _beyond(what, rows=rows, V=V, history=most, bias=n_bias, mask=n_masks)
+    if (n_bias == 0 and bias is not None) or (n_masks == 0 and mask is not None):
+        raise ValueError("%s: a table of biases or masks that has no rows" % what)  # (it has no address either, and would count as no rule)
     rules.history_stride, rules.n_bias, rules.n_masks = most, n_bias, n_masks
     if history_len is not None:
         _dense(what, "history_len", history_len, i32, one)

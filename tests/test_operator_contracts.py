@@ -201,3 +201,11 @@ def test_calls_without_rows(anywhere):
     assert binding.op_adjust_logits(z(2, 0, 100)).shape == (2, 0, 100)
     with pytest.raises(ValueError):
         binding.op_adjust_logits(logits, history=z(1, 5, dtype=I32))
+
+
+def test_tables_without_rows(anywhere):
+    # an empty table has no address, which the library takes for no rule at all: where every token was to be forbidden, all would be allowed
+    z = anywhere
+    for rule in (dict(mask=z(0, 4, dtype=I32)), dict(bias=z(0, 100))):
+        with pytest.raises(ValueError, match="no rows"):
+            binding.op_adjust_logits(z(2, 100), **rule)
