@@ -1124,7 +1124,11 @@ Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, 
     Plan p;
     const int group = H / Hkv;
     const int64_t rows = ceil_div64((int64_t)N * group, B);  // of a sequence and key head, on average
-    if (dtype == GR4AD_BF16 && dh >= 32 && (rows >= 48 || (dh == 128 && rows > 16))) p.rows = rows > 128 && dh > 32 ? kFlashRows : kHalfFlashRows;  // (a tile of 32 columns is one load for each of four wavefronts)
+    // Rows share staged keys where there are more than two tiles of 32, or one of 16 with 128 columns (bf16; 8 key heads of 4 heads each; captured, us, not staged | staged.  64 columns,
+    // 64 rows of a sequence: 4 sequences of 8000 keys 30.0 | 32.0, 32 of 2000 42.2 | 44.6; 96 rows: 44.6 | 33.3, 59.1 | 50.1.  128 columns, 32 rows: 42.1 | 37.8, 89.6 | 58.8, but 4 of 2000, which
+    // are latency, 24.1 | 35.5).  Tiles of 256 rows halve the reads of the keys and tiles of 128 end earlier (128 columns, 128 rows | 256: 4 sequences of 8000 keys, 2048 rows 275 | 267; 32 of 2000
+    // 581 | 600; 4 of 2000, 144 rows 42 | 50).
+    if (dtype == GR4AD_BF16 && dh >= 32 && rows > (dh == 128 ? 16 : 64)) p.rows = rows > 128 && dh > 32 ? kFlashRows : kHalfFlashRows;  // (a tile of 32 columns is one load for each of four wavefronts)
     else p.rows = rows <= 16 ? 16 : 32;
     p.tiles = tiles_of(N, B, group, p.rows);
     p.join_tiles = tiles_of(N, B, group, kRows);
@@ -1132,8 +1136,9 @@ Plan plan_of(gr4ad_dtype dtype, int B, int N, int H, int Hkv, int dh, int page, 
     // Workgroups enough to fill the chip (counted as if all sequences had the same number of rows): one per compute unit for tiles of 256 rows, two for the
     // others (tiles of 32 rows, 832 of them: 102 us alone, 113 in halves with their join); with tiles of 16 rows, which stand for many sequences of their own
     // lengths, four where that many are near (512 of up to 8192 keys: alone 256 us, in halves 224, in quarters 236; 16 of 131072 keys in 16 parts 176 us, in 32 parts
-    // 172, in 64 parts 190).  A part has 256 keys at least (1024 of the staged kinds), and a tile of 16 rows with 256 KB of keys and values at most stays whole: the parts would wait
-    // longer for their join than they save (one row of 777 keys, calls in a row: bf16 of 64 columns 9.8 us against 14.7; fp32 of 128, twice beyond: 23.4 against 15.2).
+    // 172, in 64 parts 190).  A part has 256 keys at least (1024 of the staged kinds), and a tile of 16 rows with 256 KB of keys and values at most stays whole: a call
+    // from a program is bound by its launches, of which parts have one more and a workspace (one row of 777 keys, calls in a row, whole | in parts: bf16 of 64 columns 9.8 | 14.7 us; fp32 of
+    // 128, twice beyond, 23.4 | 15.2.  Captured, bf16 of 64 columns: 512 keys 8.7 | 9.6, 777 10.2 | 9.4, 1024 12.1 | 10.0, 2048 19.1 | 11.3).
     const int64_t blocks = (int64_t)B * ceil_div64(rows, p.rows) * Hkv, enough = p.rows == kFlashRows ? 256 : p.rows == 16 && blocks >= 256 ? 1024 : 512, least = flash ? 1024 : 256;
     int64_t keys = (int64_t)max_pages * page;
     if (window && (int64_t)window + sinks + 64 < keys) keys = (int64_t)window + sinks + 64;
