@@ -295,8 +295,10 @@ int gr4ad_op_gather_rows(gr4ad_dtype dtype, const void *src_dev, const int32_t *
  *   out            [N, H, dh] dtype, dense
  *   workspace_dev  gr4ad_op_paged_attention_workspace_bytes bytes of scratch (0: none), not shared by calls that overlap in time
  * out, the workspace and pages that receive new tokens share no byte with any other buffer of the call (EINVAL).
- * float32 sums, maxima and normalisers; in bf16, long chunks round the softmax's weights once, as operands of the product with the values, and other
- * rows enter them as two bf16 numbers.  Same bits from run to run; a row's bits may depend on the batch it is in (which decides how its keys are split).
+ * float32 sums, maxima and normalisers.  In bf16 the softmax's weights enter the product with the values as two bf16 numbers each, and the result carries its own rounding
+ * alone; but in a call whose sequences have more than 64 rows (new tokens times heads of a group, N * H / H_kv / B) on average, more than 16 with 128 columns, they enter
+ * rounded to one bf16 number (head widths from 32 on): about 0.0022 of a row's norm off instead of 0.0017.  A key whose score is minus infinity counts as one that is not seen.
+ * Same bits from run to run; a row's bits may depend on the batch it is in (which decides how its keys are split).
  * B, N >= 1; max_pages * page_size, N * H and B * H_kv at most 2^30, H * dh below 2^31, and no more workgroups
  * than one launch takes (N * H / 16 + B * H_kv up to 2^22 always fit); head widths 16, 32, 64, 128; page_size a power of two from 16 to 1024; q, k_new and v_new with their rows, out, both page arrays and the
  * workspace 16-byte aligned.

@@ -42,6 +42,34 @@ def test_work_counted_for_attention(profile, new, dtype, kind):
     assert got["launches"] == 1 and got["flops"] == 0 and got["bytes"] == 0
 
 
+@pytest.mark.parametrize("dtype,dh,group,news,staged", [
+    (torch.bfloat16, 64, 4, [16, 16], False), (torch.bfloat16, 64, 4, [32, 1], True), (torch.bfloat16, 32, 1, [64], False), (torch.bfloat16, 32, 1, [65], True), (torch.bfloat16, 128, 16, [1, 1], False),
+    (torch.bfloat16, 128, 17, [1], True), (torch.bfloat16, 128, 4, [1] * 3 + [40], True), (torch.bfloat16, 16, 4, [100], False), (torch.float32, 128, 4, [100], False),
+])
+def test_when_weights_are_rounded_once(profile, dtype, dh, group, news, staged):
+    # The documented rule: bf16, 32 columns or more, and more than 64 rows (tokens times heads of a group) of a sequence on average, with 128 columns more than 16.
+    H_kv, page, B, n = 2, 16, len(news), 128
+    H, N, g = H_kv * group, sum(news), torch.Generator().manual_seed(dh + group)
+    q, k, v = (torch.randn(*shape, generator=g).to(dtype) for shape in ((N, H, dh), (8 * B, H_kv, page, dh), (8 * B, H_kv, dh, page)))
+    start = torch.tensor([0] + news).cumsum(0).to(torch.int32)
+    out = binding.op_paged_attention(q.cuda(), k.cuda(), v.cuda(), torch.arange(8 * B, dtype=torch.int32, device="cuda").view(B, 8), start.cuda(), torch.full((B,), n, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    assert set(profile()) == {"paged_attention_staged" if staged else "paged_attention"}
+    half = torch.finfo(dtype).eps / 2
+    for b, m in enumerate(news):
+        keys = k[8 * b:8 * b + 8].double().transpose(1, 2).flatten(0, 1).repeat_interleave(group, 1)                       # [n, H, dh]
+        values = v[8 * b:8 * b + 8].double().permute(0, 3, 1, 2).flatten(0, 1).repeat_interleave(group, 1)
+        for i in range(m):
+            row, p = int(start[b]) + i, n - m + i
+            x = (q[row].double()[None] * keys[:p + 1]).sum(-1) * dh ** -0.5
+            w = torch.softmax(x, 0)[..., None]
+            want, mag = (w * values[:p + 1]).sum(0), (w * values[:p + 1].abs()).sum(0)
+            # float32: scores of dh terms and their exponentials, sums of p + 1; the result's rounding; a weight as one bf16 number is off by 2^-8, as two by 2^-16 of itself
+            score = (dh + 8) * 2.0 ** -24 * (q[row].double().abs()[None] * keys[:p + 1].abs()).sum(-1).amax(0)[:, None] * dh ** -0.5
+            tol = (2 * score + (p + 17) * 2.0 ** -24 + (0 if dtype == torch.float32 else 2.0 ** -8 if staged else 2.0 ** -16)) * mag + half * want.abs() * (1 + 2.0 ** -7)
+            assert ((out[row].cpu().double() - want).abs() <= tol).all()
+
+
 def random_e4m3(g, *shape):
     b = torch.randint(0, 256, shape, generator=g, dtype=torch.uint8)
     b[(b & 0x7F) == 0x7F] = 0x3A
@@ -73,3 +101,30 @@ def test_products_over_many_blocks(profile, M, N, K, kind, out):
     tol = (2e-4 + nb * 2.0 ** -24) * mag + want.abs() * torch.finfo(out).eps / 2 * (1 + 2e-4) + 2.0 ** -24
     far = (C.cpu()[rows][:, cols].double() - want).abs() - tol
     assert (far <= 0).all(), float((far / mag).max())
+
+
+@pytest.mark.parametrize("dtype,m", [(torch.float32, 1), (torch.float32, 40), (torch.bfloat16, 1), (torch.bfloat16, 12), (torch.bfloat16, 40)])
+def test_scores_of_minus_infinity(dtype, m):
+    # such keys count as not seen; a row that sees no others is zero
+    H, H_kv, dh, page, n = 4, 2, 64, 16, 90
+    g = torch.Generator().manual_seed(m)
+    q, k, v = (torch.randn(*shape, generator=g).to(dtype) for shape in ((m, H, dh), (6, H_kv, page, dh), (6, H_kv, dh, page)))
+    q[..., 5] = 1.0
+    table, start, lens = torch.arange(6, dtype=torch.int32).view(1, 6).cuda(), torch.tensor([0, m], dtype=torch.int32).cuda(), torch.tensor([n], dtype=torch.int32).cuda()
+    gone = torch.rand(96, generator=g) < 0.5
+    for every in (False, True):
+        dead = gone | every
+        kk = k.transpose(1, 2).reshape(96, H_kv, dh).clone()
+        kk[dead, :, 5] = -float("inf")
+        out = binding.op_paged_attention(q.cuda(), kk.view(6, page, H_kv, dh).transpose(1, 2).contiguous().cuda(), v.cuda(), table, start, lens).cpu().double()
+        if every:
+            assert not out.any()
+            continue
+        vv = v.permute(0, 3, 1, 2).reshape(96, H_kv, dh).double().repeat_interleave(2, 1)
+        for i in range(m):
+            seen = ~dead & (torch.arange(96) <= n - m + i)
+            x = (q[i].double()[None] * kk[seen].double().repeat_interleave(2, 1)).sum(-1) * dh ** -0.5
+            w = torch.softmax(x, 0)[..., None]
+            # scores of 64 terms of magnitude 3 at most on average, 1e-4 of them for float32 sums; bf16: a weight's and the result's rounding
+            tol = 1e-4 + (2.0 ** -7 if dtype == torch.bfloat16 else 0) * (w * vv[seen].abs()).sum(0)
+            assert ((out[i] - (w * vv[seen]).sum(0)).abs() <= tol).all()
