@@ -285,11 +285,12 @@ int gr4ad_op_gather_rows(gr4ad_dtype dtype, const void *src_dev, const int32_t *
  *
  *   cache          where keys and values live (the struct is host memory).  Position j of sequence b lies on page page_table[b, j / page_size], slot
  *                  j % page_size.  Keys of a page are [H_kv, page_size, dh], values [H_kv, dh, page_size] (transposed).  Sequences may share pages.
- *                  A page number outside [0, n_pages): the positions on it count as absent.
+ *                  A page number outside [0, n_pages): the positions on it count as absent.  Entries behind a
+ *                  sequence's length may name any page.
  *   q              [N, H, dh] dtype, rows q_stride elements apart (a part of a wider row is fine)
  *   k_new, v_new   [N, H_kv, dh] dtype, rows kv_stride elements apart: written into their pages first; both NULL if the pages hold them already.
  *                  No two new tokens may lie on one slot of one page, and a page that receives new tokens stands at one place of one sequence's
- *                  table (pages that a call only reads may stand anywhere)
+ *                  table, within its length (pages that a call only reads may stand anywhere)
  *   q_start        [B+1] int32 device, ascending from >= 0 to <= N; rows in no sequence are left as they are.  seq_len [B] int32 device, at most
  *                  max_pages * page_size (clamped).  Tokens at negative positions (seq_len[b] < m_b) are neither written nor see anything
  *   out            [N, H, dh] dtype, dense

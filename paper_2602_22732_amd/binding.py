@@ -454,7 +454,8 @@ def _ptr(t):
 def op_paged_attention(q, k_pages, v_pages, page_table, q_start, seq_len, k_new=None, v_new=None, scale=None, window=0, sinks=0, out=None, workspace=None, stream=None):
     """gr4ad_op_paged_attention: q [N,H,dh] (rows may be strided), k_pages [n_pages,H_kv,page_size,dh], v_pages [n_pages,H_kv,dh,page_size], page_table
     [B,max_pages], q_start [B+1], seq_len [B] int32; k_new, v_new [N,H_kv,dh] are written into their pages first (pages that no other sequence of the call
-    has in its table).  scale: 1/sqrt(dh) if None."""
+    has in its table, within its length).  scale: 1/sqrt(dh) if None.  out: if None a new tensor, in which rows of no sequence are not set.  workspace: any dense tensor that is
+    large enough; if None allocated."""
     what = "op_paged_attention"
     at = _place(what, q, stream, (k_pages, v_pages, page_table, q_start, seq_len, k_new, v_new, out, workspace))
     if at is not None:

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2602_22732_amd import binding
+from test_gpu_paged_attention import Case, check, same
 
 pytestmark = pytest.mark.gpu
 
@@ -128,3 +129,27 @@ def test_scores_of_minus_infinity(dtype, m):
             # scores of 64 terms of magnitude 3 at most on average, 1e-4 of them for float32 sums; bf16: a weight's and the result's rounding
             tol = 1e-4 + (2.0 ** -7 if dtype == torch.bfloat16 else 0) * (w * vv[seen].abs()).sum(0)
             assert ((out[i] - (w * vv[seen]).sum(0)).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("dtype,new", [("f32", [1, 1, 1]), ("f32", [3, 40, 1]), ("bf16", [1, 1, 1]), ("bf16", [3, 40, 1]), ("bf16", [100, 90, 120])])
+def test_padded_tables(dtype, new):
+    # entries behind a sequence's length may name any page, such as one that takes another sequence's new tokens in the same call
+    for page in (16, 64):
+        c = Case(dtype, 64, 4, 2, page, new=new, lens=[300, 130, 121], seed=31)
+        busy = int(c.table[0, 299 // page])
+        for b, n in enumerate(c.lens):
+            c.table[b, -(-n // page):] = busy
+        check(c)
+        check(c, window=70, sinks=3)
+
+
+@pytest.mark.parametrize("dtype,new", [("f32", [2, 1]), ("bf16", [2, 1]), ("bf16", [90, 80])])
+def test_lengths_beyond_the_table(dtype, new):
+    # counted as the table's: the new tokens are the last of the positions that it has
+    c = Case(dtype, 64, 4, 2, 16, new=new, lens=[320, 100], seed=32)
+    want, tol = c.expected()
+    args = [t.cuda() for t in (c.q, c.k, c.v, c.table, torch.tensor(c.starts, dtype=torch.int32))]
+    out = binding.op_paged_attention(*args, torch.tensor([2 ** 31 - 1, 100], dtype=torch.int32).cuda(), k_new=c.k_new.cuda(), v_new=c.v_new.cuda())
+    assert ((out.cpu().double() - want).abs() <= tol).all()
+    k, v = c.after()
+    assert same(args[1].cpu(), k) and same(args[2].cpu(), v)
