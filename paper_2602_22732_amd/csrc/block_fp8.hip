@@ -643,7 +643,7 @@ template <int TM, int TN> int launch_tile(const BlockGemm &g, hipStream_t st) {
 }
 
 template <int MG> int launch_few(const BlockGemm &g, hipStream_t st) {
-    // as many column groups per workgroup as leave 256 workgroups
+    // as many column groups per workgroup as leave 256 workgroups (64 rows x 16384 x 8192: one 79 us, four 38)
     const int groups = (g.N + 15) / 16, each = MG == 1 || groups < 512 ? 1 : groups < 1024 ? 2 : 4;
     const dim3 grid((groups + each - 1) / each);
     if (!launchable(grid.x, 512)) return too_many_tiles(g);
@@ -656,9 +656,12 @@ template <int MG> int launch_few(const BlockGemm &g, hipStream_t st) {
     return GR4AD_OK;
 }
 
-// The variants by size.  Up to 64 rows every weight is read once by whoever needs it.  Then the time is the rounds of tiles: a compute unit holds two workgroups of
+// The variants by size.  Up to 64 rows every weight is read once by whoever needs it (64 rows, captured, in tiles of 64 instead: x 4096 x 4096 11.8 us against 14.1, x 8192 x 8192 25.2
+// against 25.3; only where a tile for every compute unit comes together are tiles faster, x 16384 x 8192 40.9 against 32.5, 16 rows 34.3 against 31.7).  Then the time is the rounds of tiles: a compute unit holds two workgroups of
 // 64 x 64 or 128 x 128 tiles and one of 256 x 256, so each size is left when it needs more rounds than the next (x 4096 x 4096, tiles of 64, 128, 256: 128 rows 15,
-// 35, 46 us; 1024 rows, two rounds of the smallest, 34, 36, 45; 2048 rows, one round of the middle ones, 65, 46, 47; 2816 rows 90, 74, 49; 4096 rows 125, 86, 60).
+// 35, 46 us; 1024 rows, two rounds of the smallest, 34, 36, 45; 2048 rows, one round of the middle ones, 65, 46, 47; 2816 rows 90, 74, 49; 4096 rows 125, 86, 60).  Rows
+// that do not start on 16 bytes take tiles of 128 from a tile per compute unit on (tiles of 64 | 128, x 5000 x 1111: 500 rows 21 | 26 us, 800 rows 32.7 | 32.4, 3000 rows 78 | 56; x 4096 x 4001:
+// 800 rows 60 | 63, 1200 rows 82 | 74).
 int launch_block_gemm(const BlockGemm &g, hipStream_t st) {
     // rows in pieces of 16 bytes (and a tile's rows within 32 bits of its first): direct loads to LDS
     const bool aligned = g.K % 16 == 0 && g.K < (1 << 23) && (uintptr_t)g.A % 16 == 0 && (uintptr_t)g.W % 16 == 0;

@@ -173,7 +173,9 @@ template <int DH> __device__ __forceinline__ float *part_row(const PagedArgs &a,
 }
 
 // One row over blocks [x0, x1), key by key: only visible keys and values are read.  The form for tiles whose sums are no numbers: where a key that
-// some rows do not see holds an infinity or a NaN, the tile's product with p = 0 would carry it into those rows.
+// some rows do not see holds an infinity or a NaN, the tile's product with p = 0 would carry it into those rows.  Rows of a wavefront go one by one, 0.35 us a key, so it
+// is the form of broken data alone: with one infinity among a sequence's first values, which every row sees, 64 sequences of 512 to 8192 keys and a token each take
+// 349 us for 224, and 1000 tokens over 8192 keys (32 heads of 128 over 8) 91 ms for 0.2.
 template <typename T, int DH, int KB>
 __device__ void plain_row(const PagedArgs &a, const Sequence &s, const Blocks &bl, int x0, int x1, int kvh, int row, int head, int p, int split) {
     const int lane = threadIdx.x % 64, page = 1 << a.page_shift;
@@ -683,8 +685,8 @@ template <typename T, int DH, int MR> __global__ __launch_bounds__(256, MR * DH 
 // swapped, which makes the eight keys a lane holds for one MFMA step consecutive; the weights are rounded to bf16 there, while their sum keeps 32 bits).
 // The matrix cores and the vector instructions of the softmax need about the same time, so a wavefront runs them side by side: the scores of tile x + 1 are
 // formed while those of tile x become weights.  (64 rows per wavefront halve the reads of LDS and do not fit the registers: 1075 us for what takes 314.)
-// bf16, 4 sequences of 1000 to 1024 new tokens among up to 8192, 32 heads of 128 columns over 8: 314 us under the tracer, 280 in a row of calls, 0.97 PFLOP/s
-// of the products that the mask leaves; the matrix cores are busy for 40 % of the cycles, the rest is the softmax's and the reads of LDS.
+// bf16, 4 sequences of 1000 to 1024 new tokens among up to 8192, 32 heads of 128 columns over 8: 314 us under the tracer, and 292 to 302 for a call among others, the
+// pages' update with it, 0.9 PFLOP/s of the products that the mask leaves; the matrix cores are busy for 40 % of the cycles, the rest is the softmax's and the reads of LDS.
 // ---------------------------------------------------------------------------------------------------------------------
 template <int DH, int NW, int SLOTS> __global__ __launch_bounds__(NW * 64, 2) void paged_flash(PagedArgs a) {
     constexpr int ROWS = NW * 32, KT = 64, KCH = DH / 8, HALF = KT * KCH, KSTEPS = DH / 16, MT = DH / 32, KI = HALF / 64 / NW, LEAD = SLOTS - 1;
